@@ -19,8 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgasloc.so")
 SOURCES = ["adamw.hip", "round_planned.hip", "round_tile_f32.hip", "round_tile_bf16.hip",
-           "reductions.hip", "stream_probe.hip", "runtime.cpp", "topology.cpp", "schedule.cpp",
-           "plan.cpp"]
+           "reductions.hip", "stream_probe.hip", "embedding.hip", "layer_norm.hip", "linear.hip",
+           "runtime.cpp", "layers.cpp", "topology.cpp", "schedule.cpp", "plan.cpp"]
 ARCH = "gfx950"
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-ffp-contract=off",

@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libgasloc.so: same names as include/gasloc.h.
+"""Thin ctypes binding of libgasloc.so: same names as include/gasloc.h and
+include/gasloc_layers.h.
 
 Argument marshalling only: torch tensors become device pointers, numpy
 arrays become host pointers, status codes become GaslocError.  Every step of
@@ -85,6 +86,19 @@ _SIGNATURES = {
     "gasloc_lr_schedule": (ctypes.c_float, [ctypes.c_float, _i64, _i64, ctypes.c_float, ctypes.c_float,
                                             ctypes.c_float]),
     "gasloc_stream_probe": (ctypes.c_int, [_i32, _i32, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _vp]),
+    "gasloc_embedding": (ctypes.c_int, [_vp, _i64, _i32, _i32, ctypes.c_float, _vp, _vp, _i32, _vp, _i64]),
+    "gasloc_embedding_grad": (ctypes.c_int, [_vp, _i64, _i32, _i32, ctypes.c_float, _vp, _vp, _i32, _vp, _i64, _vp,
+                                             _i64, _i32, _vp, ctypes.c_size_t]),
+    "gasloc_embedding_grad_workspace": (ctypes.c_int, [_vp, _i32, _vp, ctypes.POINTER(ctypes.c_size_t)]),
+    "gasloc_layer_norm": (ctypes.c_int, [_vp, _i64, _i64, _i32, ctypes.c_float, _vp, _vp, _i64, _i32, _vp, _i64, _vp]),
+    "gasloc_layer_norm_grad": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _i64,
+                                              _vp, _i64, _i32, _vp, ctypes.c_size_t]),
+    "gasloc_layer_norm_grad_workspace": (ctypes.c_int, [_vp, _i32, _vp, ctypes.POINTER(ctypes.c_size_t)]),
+    "gasloc_linear": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i64]),
+    "gasloc_linear_grad_input": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i64]),
+    "gasloc_linear_grad_weight": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _i32, _vp, _i64,
+                                                 _i32, _vp, ctypes.c_size_t]),
+    "gasloc_linear_grad_weight_workspace": (ctypes.c_int, [_vp, _i32, _i32, _vp, ctypes.POINTER(ctypes.c_size_t)]),
     "gasloc_last_error": (ctypes.c_char_p, [_vp]),
     "gasloc_build_info": (ctypes.c_char_p, []),
     "gasloc_destroy": (None, [_vp]),
@@ -321,6 +335,100 @@ def gasloc_stream_probe(reads_f32, reads_bf16, writes_f32, writes_bf16, src, dst
     _check(st)
 
 
+# Layers over the workers' rows (include/gasloc_layers.h).  row_ptr: n + 1 host numbers; activations, tokens,
+# gradients and workspaces: torch device tensors (or addresses).
+
+def _act(dtype):
+    """gasloc_dtype of an activation given by name, code or torch dtype."""
+    if dtype in ("bf16", GASLOC_BF16) or str(dtype) == "torch.bfloat16":
+        return GASLOC_BF16
+    if dtype in ("f32", GASLOC_F32) or str(dtype) == "torch.float32":
+        return GASLOC_F32
+    raise ValueError("activations are f32 or bf16, not %s" % (dtype,))
+
+
+def gasloc_embedding(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, out, out_ld):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_embedding(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
+                                      _act(dtype), _dev(out), int(out_ld)), ctx)
+    del keep
+
+
+def gasloc_embedding_grad(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, dout, dout_ld, grads, grad_ld,
+                          accumulate, workspace, workspace_bytes):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_embedding_grad(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
+                                           _act(dtype), _dev(dout), int(dout_ld), _dev(grads), int(grad_ld),
+                                           int(accumulate), _dev(workspace), int(workspace_bytes)), ctx)
+    del keep
+
+
+def gasloc_embedding_grad_workspace(ctx, width, row_ptr):
+    keep, rp = _host(row_ptr, np.int64)
+    out = ctypes.c_size_t()
+    _check(library().gasloc_embedding_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
+    del keep
+    return out.value
+
+
+def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out, out_ld, stats=None):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_layer_norm(ctx, int(gain), int(bias), int(width), float(eps), rp, _dev(x), int(x_ld),
+                                       _act(dtype), _dev(out), int(out_ld), _dev(stats)), ctx)
+    del keep
+
+
+def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout, dout_ld, dtype, dx, dx_ld, grads,
+                           grad_ld, accumulate, workspace, workspace_bytes):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_layer_norm_grad(ctx, int(gain), int(bias), int(width), rp, _dev(x), int(x_ld),
+                                            _dev(stats), _dev(dout), int(dout_ld), _act(dtype), _dev(dx), int(dx_ld),
+                                            _dev(grads), int(grad_ld), int(accumulate), _dev(workspace),
+                                            int(workspace_bytes)), ctx)
+    del keep
+
+
+def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
+    keep, rp = _host(row_ptr, np.int64)
+    out = ctypes.c_size_t()
+    _check(library().gasloc_layer_norm_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
+    del keep
+    return out.value
+
+
+def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtype, out, out_ld):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_linear(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x), int(x_ld),
+                                   _act(dtype), _dev(out), int(out_ld)), ctx)
+    del keep
+
+
+def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, dout, dout_ld, dtype, dx, dx_ld):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_linear_grad_input(ctx, int(weight), int(out_features), int(in_features), rp, _dev(dout),
+                                              int(dout_ld), _act(dtype), _dev(dx), int(dx_ld)), ctx)
+    del keep
+
+
+def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dout, dout_ld, dtype, grads,
+                              grad_ld, accumulate, workspace, workspace_bytes):
+    keep, rp = _host(row_ptr, np.int64)
+    _check(library().gasloc_linear_grad_weight(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x),
+                                               int(x_ld), _dev(dout), int(dout_ld), _act(dtype), _dev(grads),
+                                               int(grad_ld), int(accumulate), _dev(workspace),
+                                               int(workspace_bytes)), ctx)
+    del keep
+
+
+def gasloc_linear_grad_weight_workspace(ctx, out_features, in_features, row_ptr):
+    keep, rp = _host(row_ptr, np.int64)
+    out = ctypes.c_size_t()
+    _check(library().gasloc_linear_grad_weight_workspace(ctx, int(out_features), int(in_features), rp,
+                                                         ctypes.byref(out)))
+    del keep
+    return out.value
+
+
 def gasloc_last_error(ctx=None):
     msg = library().gasloc_last_error(ctx)
     return msg.decode() if msg else ""
@@ -364,6 +472,41 @@ def alloc_buffers(n, P, param_dtype="f32", device="cuda", with_u=True, with_zp=T
     u = torch.empty((n, ld), dtype=torch.float32, device=device) if with_u else None
     zp = torch.empty((n, ld), dtype=torch.float32, device=device) if with_zp else None
     return dict(x=x, y=y, m=m, v=v, u=u, zp=zp, ld=ld)
+
+
+def _rows_of(name, t, rows, cols, dtype, device):
+    """Checks that tensor t can hold (at least) `rows` rows of `cols` elements, each contiguous; returns its row length."""
+    if t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s on %s, not %s on %s" % (name, dtype, device, t.dtype, t.device))
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or \
+            (t.numel() > 0 and cols > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be at least %d rows of %d contiguous elements, not %s with strides %s"
+                         % (name, rows, cols, tuple(t.shape), tuple(t.stride())))
+    return t.stride(0) if t.shape[0] > 1 else cols  # the stride of a single row means nothing
+
+
+class _OnStream:
+    """Runs a call on the context's stream between the current stream's work: what the current
+    stream has enqueued is seen by the call, and what it enqueues next sees the results."""
+
+    def __init__(self, stream, tensors):
+        self.stream, self.tensors = stream, tensors
+
+    def __enter__(self):
+        import torch
+
+        self.current = torch.cuda.current_stream(self.stream.device)
+        self.other = self.current.cuda_stream != self.stream.cuda_stream
+        if self.other:
+            self.stream.wait_stream(self.current)
+            for t in self.tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+    def __exit__(self, *exc):
+        if self.other:
+            self.current.wait_stream(self.stream)
+        return False
 
 
 class GASLoC:
@@ -423,6 +566,147 @@ class GASLoC:
 
     def replica_mean(self, out):
         gasloc_replica_mean(self.ctx, out)
+
+    # -- layers (include/gasloc_layers.h): x, dout, tokens hold the rows of all workers, worker i's at
+    # row_ptr[i] .. row_ptr[i + 1] - 1; weights start at a column of every worker's row.  Results go to
+    # the tensors given, or to new ones.  The calls run on the context's stream, in order with the current one.
+
+    def _layer(self, row_ptr):
+        rp = np.ascontiguousarray(row_ptr, dtype=np.int64)
+        if rp.shape != (self.n + 1,):
+            raise ValueError("row_ptr needs %d numbers" % (self.n + 1))
+        return rp, int(rp[-1]), self.bufs["x"].device
+
+    def _new(self, t, rows, cols, dtype):
+        import torch
+
+        return torch.empty((rows, cols), dtype=dtype, device=self.bufs["x"].device) if t is None else t
+
+    def _workspace(self, workspace, need):
+        import torch
+
+        if workspace is None:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=self.bufs["x"].device)
+        if workspace.device != self.bufs["x"].device or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous on %s" % self.bufs["x"].device)
+        return workspace, workspace.numel() * workspace.element_size()
+
+    def _tokens(self, tokens, rows, device):
+        import torch
+
+        if tokens.dtype != torch.int32 or tokens.device != device or tokens.dim() != 1 or tokens.shape[0] < rows or \
+                (tokens.shape[0] > 1 and tokens.stride(0) != 1):
+            raise ValueError("tokens must be at least %d contiguous int32 on %s" % (rows, device))
+
+    def _grads(self, grads, device):
+        import torch
+
+        if grads.dim() != 2 or grads.shape[0] != self.n or grads.shape[1] < self.P:
+            raise ValueError("grads must be [%d, >= %d]" % (self.n, self.P))
+        ld = _rows_of("grads", grads, self.n, grads.shape[1], torch.float32, device)
+        return ld if self.n > 1 else (ld + 3) // 4 * 4
+
+    def embedding(self, table, vocab, width, tokens, row_ptr, scale=1.0, dtype=None, out=None):
+        """out[t] = scale * E_i[tokens[t]], E_i the [vocab, width] table at column `table` of worker i's row;
+        tokens outside the table give zeros.  dtype: "f32" or "bf16" (that of out; default: the parameters')."""
+        import torch
+
+        rp, rows, device = self._layer(row_ptr)
+        if out is not None:
+            dt = out.dtype
+        else:
+            dt = torch.bfloat16 if _act(self.bufs["x"].dtype if dtype is None else dtype) == GASLOC_BF16 else torch.float32
+        out = self._new(out, rows, width, dt)
+        ld = _rows_of("out", out, rows, width, dt, device)
+        self._tokens(tokens, rows, device)
+        with _OnStream(self.stream, (tokens, out)):
+            gasloc_embedding(self.ctx, table, vocab, width, scale, rp, tokens, dt, out, ld)
+        return out
+
+    def embedding_grad(self, table, vocab, width, tokens, row_ptr, dout, grads, scale=1.0, accumulate=False,
+                       workspace=None):
+        """Writes (or adds) the table's gradient into its columns of grads [n, >= P]."""
+        rp, rows, device = self._layer(row_ptr)
+        ld = _rows_of("dout", dout, rows, width, dout.dtype, device)
+        gld = self._grads(grads, device)
+        self._tokens(tokens, rows, device)
+        ws, size = self._workspace(workspace, gasloc_embedding_grad_workspace(self.ctx, width, rp))
+        with _OnStream(self.stream, (tokens, dout, grads, ws)):
+            gasloc_embedding_grad(self.ctx, table, vocab, width, scale, rp, tokens, dout.dtype, dout, ld, grads, gld,
+                                  bool(accumulate), ws, size)
+
+    def layer_norm(self, gain, bias, width, x, row_ptr, eps=1e-5, out=None, stats=None):
+        """(out, stats): the normalised rows (gain and bias at these columns; bias None: none) and every
+        row's (mean, rstd) for layer_norm_grad.  out may be x."""
+        import torch
+
+        rp, rows, device = self._layer(row_ptr)
+        x_ld = _rows_of("x", x, rows, width, x.dtype, device)
+        out = self._new(out, rows, width, x.dtype)
+        ld = _rows_of("out", out, rows, width, x.dtype, device)
+        stats = self._stats(stats, rows, device)
+        with _OnStream(self.stream, (x, out, stats)):
+            gasloc_layer_norm(self.ctx, gain, -1 if bias is None else bias, width, eps, rp, x, x_ld, x.dtype, out, ld,
+                              stats)
+        return out, stats
+
+    def _stats(self, stats, rows, device):
+        import torch
+
+        stats = self._new(stats, rows, 2, torch.float32)
+        if _rows_of("stats", stats, rows, 2, torch.float32, device) != 2 and rows > 1:
+            raise ValueError("stats must be contiguous")
+        return stats
+
+    def layer_norm_grad(self, gain, bias, width, x, row_ptr, stats, dout, grads, dx=None, accumulate=False,
+                        workspace=None):
+        """dx; the gradients of gain and bias go into (or are added to) their columns of grads.  dx may be
+        dout or x."""
+        rp, rows, device = self._layer(row_ptr)
+        x_ld = _rows_of("x", x, rows, width, x.dtype, device)
+        d_ld = _rows_of("dout", dout, rows, width, x.dtype, device)
+        dx = self._new(dx, rows, width, x.dtype)
+        ld = _rows_of("dx", dx, rows, width, x.dtype, device)
+        stats = self._stats(stats, rows, device)
+        gld = self._grads(grads, device)
+        ws, size = self._workspace(workspace, gasloc_layer_norm_grad_workspace(self.ctx, width, rp))
+        with _OnStream(self.stream, (x, stats, dout, dx, grads, ws)):
+            gasloc_layer_norm_grad(self.ctx, gain, -1 if bias is None else bias, width, rp, x, x_ld, stats, dout, d_ld,
+                                   x.dtype, dx, ld, grads, gld, bool(accumulate), ws, size)
+        return dx
+
+    def linear(self, weight, out_features, in_features, x, row_ptr, out=None):
+        """out[t] = W_i x[t], W_i the [out_features, in_features] matrix at column `weight` of worker i's row."""
+        rp, rows, device = self._layer(row_ptr)
+        x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
+        out = self._new(out, rows, out_features, x.dtype)
+        ld = _rows_of("out", out, rows, out_features, x.dtype, device)
+        with _OnStream(self.stream, (x, out)):
+            gasloc_linear(self.ctx, weight, out_features, in_features, rp, x, x_ld, x.dtype, out, ld)
+        return out
+
+    def linear_grad_input(self, weight, out_features, in_features, dout, row_ptr, dx=None):
+        """dx[t] = W_i^T dout[t]."""
+        rp, rows, device = self._layer(row_ptr)
+        d_ld = _rows_of("dout", dout, rows, out_features, dout.dtype, device)
+        dx = self._new(dx, rows, in_features, dout.dtype)
+        ld = _rows_of("dx", dx, rows, in_features, dout.dtype, device)
+        with _OnStream(self.stream, (dout, dx)):
+            gasloc_linear_grad_input(self.ctx, weight, out_features, in_features, rp, dout, d_ld, dout.dtype, dx, ld)
+        return dx
+
+    def linear_grad_weight(self, weight, out_features, in_features, x, dout, row_ptr, grads, accumulate=False,
+                           workspace=None):
+        """Writes (or adds) sum_t dout[t] x[t]^T of every worker into its columns of grads."""
+        rp, rows, device = self._layer(row_ptr)
+        x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
+        d_ld = _rows_of("dout", dout, rows, out_features, x.dtype, device)
+        gld = self._grads(grads, device)
+        ws, size = self._workspace(
+            workspace, gasloc_linear_grad_weight_workspace(self.ctx, out_features, in_features, rp))
+        with _OnStream(self.stream, (x, dout, grads, ws)):
+            gasloc_linear_grad_weight(self.ctx, weight, out_features, in_features, rp, x, x_ld, dout, d_ld, x.dtype,
+                                      grads, gld, bool(accumulate), ws, size)
 
     def counters(self):
         """(k, stepped, rounds_done): per-worker AdamW step counts, which workers
