@@ -19,7 +19,7 @@
  *     step since the last round, else row i of x.  Which of the two is decided
  *     when the call is made, also for a call that is recorded in a graph.
  *   - Activations: device memory, row t at offset t * ld elements (ld >= the
- *     row's length, < 2^22), dtype GASLOC_F32 or GASLOC_BF16, aligned to the
+ *     row's length, < 2^21), dtype GASLOC_F32 or GASLOC_BF16, aligned to the
  *     element.  Types go together as (parameters, activations) = (F32, F32),
  *     (F32, BF16), (BF16, BF16); EINVAL for F32 activations with BF16
  *     parameters.

@@ -27,6 +27,10 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-ffp-contract=off",
           "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 HIP = ["-x", "hip", "--offload-arch=" + ARCH, "-fno-gpu-rdc"]
 DEVICE_ONLY = ["--cuda-device-only", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# linear.hip: accumulators stay in vector registers.  Left to itself the compiler keeps them in
+# accumulation registers and copies most of them around in every step of the loop (150 copies beside 64
+# matrix instructions), or spills.
+EXTRA = {"linear.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
@@ -70,7 +74,7 @@ def _compile(src, verbose, info):
         return _run(HOST_CXX + COMMON + ['-DGASLOC_BUILD_INFO="%s"' % info, "-c", path, "-o", obj], verbose) or obj
     if src.endswith(".hip"):
         fatbin = device_binary(src)
-        _run(["hipcc"] + COMMON + HIP + DEVICE_ONLY + ["-c", path, "-o", fatbin], verbose)
+        _run(["hipcc"] + COMMON + HIP + DEVICE_ONLY + EXTRA.get(src, []) + ["-c", path, "-o", fatbin], verbose)
         _run(["hipcc"] + COMMON + HIP + ["--cuda-host-only", "-Xclang", "-fcuda-include-gpubinary", "-Xclang",
                                          fatbin, "-c", path, "-o", obj], verbose)
     else:  # host-only C++ against the HIP runtime API

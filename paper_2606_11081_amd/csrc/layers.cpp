@@ -24,7 +24,7 @@ using gasloc::Spans;
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;
-constexpr int64_t kMaxLd = int64_t(1) << 22;
+constexpr int64_t kMaxLd = int64_t(1) << 21;
 
 // Nothing but a status leaves the library: building a message may run out of memory.
 template <typename F>
@@ -68,7 +68,7 @@ std::string check_columns(const gasloc_ctx& c, const char* what, int64_t begin, 
 std::string check_act(const char* what, const void* p, int64_t ld, int64_t cols, int64_t rows, int32_t dtype) {
   if (rows > 0 && !p) return format("%s must not be NULL", what);
   if (reinterpret_cast<uintptr_t>(p) % param_bytes(dtype) != 0) return format("%s is not aligned to its elements", what);
-  if (ld < cols || ld >= kMaxLd) return format("%s: row length must be in [%lld, 2^22)", what, (long long)cols);
+  if (ld < cols || ld >= kMaxLd) return format("%s: row length must be in [%lld, 2^21)", what, (long long)cols);
   return "";
 }
 
@@ -207,8 +207,9 @@ std::string check_weight(const gasloc_ctx& c, int64_t weight, int32_t out_featur
 }
 
 // Tiles of every worker's product; false if there are too many for one launch.
-bool linear_tiles(int n, const int64_t* row_ptr, const gasloc::LinearArgs& a, gasloc::LinearPass pass, Spans* tiles) {
-  const auto cut = [](int64_t v) { return (v + gasloc::kLinearTile - 1) / gasloc::kLinearTile; };
+bool linear_tiles(int n, const int64_t* row_ptr, const gasloc::LinearArgs& a, gasloc::LinearPass pass, int tile,
+                  Spans* tiles) {
+  const auto cut = [tile](int64_t v) { return (v + tile - 1) / tile; };
   int64_t at = 0;
   tiles->begin[0] = 0;
   for (int i = 0; i < n; ++i) {
@@ -227,10 +228,20 @@ gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPas
   a->w = live_rows(*c);
   a->n = c->n;
   a->rows = row_spans(c->n, row_ptr);
-  if (!linear_tiles(c->n, row_ptr, *a, pass, &a->tiles)) return fail(c, GASLOC_EINVAL, "product too large for one launch");
+  const bool vec = vector_columns(*c, a->weight) && (!a->x || vector_rows(a->x, a->x_ld, a->in_features, dtype)) &&
+                   (!a->dout || vector_rows(a->dout, a->dout_ld, a->out_features, dtype)) &&
+                   (!a->out || vector_rows(a->out, a->out_ld, 0, dtype)) && a->in_features % 8 == 0 &&
+                   a->out_features % 8 == 0;
+  int tile = vec && dtype == GASLOC_BF16 ? 256 : 128;
+  bool fits = linear_tiles(c->n, row_ptr, *a, pass, tile, &a->tiles);
+  if (fits && tile == 256 && a->tiles.begin[c->n] < 2 * c->cus) {
+    tile = 128;
+    fits = linear_tiles(c->n, row_ptr, *a, pass, tile, &a->tiles);
+  }
+  if (!fits) return fail(c, GASLOC_EINVAL, "product too large for one launch");
   if (a->tiles.begin[c->n] == 0) return GASLOC_OK;
   DeviceGuard guard(c->device);
-  HIP_TRY(c, gasloc::launch_linear(*a, pass, c->hp.param_dtype, dtype, c->stream));
+  HIP_TRY(c, gasloc::launch_linear(*a, pass, c->hp.param_dtype, dtype, tile, vec, c->stream));
   return GASLOC_OK;
 }
 

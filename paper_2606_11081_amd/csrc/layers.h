@@ -147,7 +147,9 @@ struct LinearArgs {
   int32_t accumulate;
   Spans rows, tiles;
 };
-constexpr int kLinearTile = 64;
-hipError_t launch_linear(const LinearArgs& a, LinearPass pass, int params, int act, hipStream_t stream);
+// tile: rows and columns of a workgroup's part of C (256, or 128: always 128 without vec and in F32); vec: every row of either operand, of C and of
+// the gradients begins on a 16-byte boundary and is a whole number of 16-byte chunks of activations.
+hipError_t launch_linear(const LinearArgs& a, LinearPass pass, int params, int act, int tile, bool vec,
+                         hipStream_t stream);
 
 }  // namespace gasloc

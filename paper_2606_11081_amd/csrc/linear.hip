@@ -1,105 +1,358 @@
-// Linear layers of every worker: products of its token rows with its weight
-// and, backward, of the gradients with the weight and with the rows.
+// Linear layers of every worker on the matrix cores: for each worker
+//   forward  out = x W^T,  input  dx = dout W,  weight  dW = dout^T x,
+// all of the form C[m][n] = sum_k A(m, k) B(n, k).
+//
+// Bound by the matrix cores where a worker has some hundred rows or more.  A
+// workgroup of four waves makes one tile of C; 64 bytes of k of both operands
+// at a time pass through LDS, in three buffers, with the loads of what follows
+// in flight in registers (fp32 weights that meet bf16 activations are rounded on
+// the way).  An operand whose rows run along k lies in LDS as [row][k] and is
+// read in 16-byte fragments; one whose rows run across k lies as [k][row] and
+// is transposed by the LDS read itself (bf16) or read by words (fp32).
 #pragma clang fp contract(off)
+
+#include <type_traits>
 
 #include "layers_device.h"
 
 namespace gasloc {
 namespace {
 
-template <int DT>
-__device__ __forceinline__ float at(const void* base, int64_t idx) {
-  if constexpr (DT == GASLOC_BF16)
-    return bf16_to_f32(static_cast<const uint16_t*>(base)[idx]);
-  else
-    return static_cast<const float*>(base)[idx];
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRowBytes = 80;   // a [row][k] row in LDS: 64 bytes and 16 that spread the rows over the banks
+constexpr int kBuffers = 3;
+constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset no buffer holds: the load gives zeros
+
+// A range of memory that loads are checked against; what lies outside reads as zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* p, int64_t bytes) {
+  const uint32_t n = bytes <= 0 ? 0u : bytes > 0x80000000ll ? 0x80000000u : static_cast<uint32_t>(bytes);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(n), 0x00027000);
 }
 
-// 64 x 64 outputs per workgroup of 256 threads, 4 x 4 each; 16 k at a time in LDS.
-template <int PASS, int PT, int AT>
-__global__ __launch_bounds__(256) void k_linear(LinearArgs a) {
-  constexpr int T = kLinearTile, K = 16;
-  __shared__ float s_a[K][T + 4], s_b[K][T + 4];
-  const int i = find_worker(a.tiles, a.n, blockIdx.x);
-  const int tile = static_cast<int>(blockIdx.x) - a.tiles.begin[i];
-  const int64_t r0 = a.rows.begin[i], count = a.rows.begin[i + 1] - r0;
-  const int64_t M = PASS == kLinearWeight ? a.out_features : count;
-  const int64_t N = PASS == kLinearForward ? a.out_features : a.in_features;
-  const int64_t depth = PASS == kLinearForward ? a.in_features : PASS == kLinearInput ? a.out_features : count;
-  const int64_t across = (N + T - 1) / T;
-  const int64_t m0 = tile / across * T, n0 = tile % across * T;
-  const void* w = live_row<PT>(a.w, i);
-  const int tm = threadIdx.x / 16 * 4, tn = threadIdx.x % 16 * 4;
-  float c[4][4] = {};
-  for (int64_t k0 = 0; k0 < depth; k0 += K) {
-    for (int e = threadIdx.x; e < K * T; e += 256) {
-      // neighbours in memory for neighbouring threads: k first where rows run along k
-      const int ka = PASS == kLinearWeight ? e / T : e % K, ma = PASS == kLinearWeight ? e % T : e / K;
-      float v = 0.0f;
-      if (k0 + ka < depth && m0 + ma < M) {
-        if constexpr (PASS == kLinearForward)
-          v = at<AT>(a.x, (r0 + m0 + ma) * a.x_ld + k0 + ka);
-        else if constexpr (PASS == kLinearInput)
-          v = at<AT>(a.dout, (r0 + m0 + ma) * a.dout_ld + k0 + ka);
-        else
-          v = at<AT>(a.dout, (r0 + k0 + ka) * a.dout_ld + m0 + ma);
-      }
-      s_a[ka][ma] = v;
-      const int kb = PASS == kLinearForward ? e % K : e / T, nb = PASS == kLinearForward ? e / K : e % T;
-      v = 0.0f;
-      if (k0 + kb < depth && n0 + nb < N) {
-        if constexpr (PASS == kLinearForward)
-          v = as_stored<AT>(at<PT>(w, a.weight + (n0 + nb) * depth + k0 + kb));
-        else if constexpr (PASS == kLinearInput)
-          v = as_stored<AT>(at<PT>(w, a.weight + (k0 + kb) * N + n0 + nb));
-        else
-          v = at<AT>(a.x, (r0 + k0 + kb) * a.x_ld + n0 + nb);
-      }
-      s_b[kb][nb] = v;
-    }
-    __syncthreads();
-    for (int k = 0; k < K; ++k) {
+// One operand of a workgroup's tile: ROWS rows (of m or n), KT of k at a time.
+// KC: rows run along k in memory.  ST: type in memory, CT: type of the product.
+// VEC: 16-byte chunks lie on 16-byte boundaries and are inside or outside as a whole.
+template <int ROWS, int THREADS, bool KC, int ST, int CT, bool VEC>
+struct Operand {
+  static constexpr int kSize = CT == GASLOC_BF16 ? 2 : 4;        // bytes of an element in LDS
+  static constexpr int kSrc = ST == GASLOC_BF16 ? 2 : 4;         // and in memory
+  static constexpr int E = 16 / kSize;                           // elements of a chunk in LDS
+  static constexpr int KT = 4 * E;                               // k per step
+  static constexpr int kChunks = ROWS * 4 / THREADS;      // chunks per thread
+  static constexpr int kWords = E * kSrc / 4;                    // words of a chunk in memory
+  static constexpr int kAcross = ROWS / E;                       // chunks of a [k][row] row
+  static constexpr int kStride = KC ? kRowBytes : ROWS * kSize + (CT == GASLOC_BF16 ? 32 : 16);
+  static constexpr int kLds = KC ? ROWS * kStride : KT * kStride;
+
+  const char* base;   // row 0, k 0 of the tile
+  int64_t ld;         // bytes between rows in memory
+  int rows, depth;    // rows inside (of ROWS), length of k
+  uint32_t off[kChunks];
+  uint32_t words[kChunks][kWords];
+
+  // p: element (first, 0) of the operand; `rows` rows from there on exist
+  __device__ __forceinline__ void start(const void* p, int64_t ld_elements, int64_t rows_left, int64_t k) {
+    base = static_cast<const char*>(p);
+    ld = ld_elements * kSrc;
+    rows = static_cast<int>(rows_left < ROWS ? rows_left : ROWS);
+    depth = static_cast<int>(k);
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) c[p][q] = fmaf(s_a[k][tm + p], s_b[k][tn + q], c[p][q]);
-      }
+    for (int j = 0; j < kChunks; ++j) {
+      const int row = row_of(j), col = col_of();
+      off[j] = static_cast<uint32_t>(row * ld + col * kSrc);
+      if (!KC && VEC && col >= rows) off[j] = kNowhere;
     }
-    __syncthreads();
   }
+  // The chunk j of this thread: its row in memory (of m or n, or of k) and its first column.
+  __device__ __forceinline__ int row_of(int j) const {
+    const int t = threadIdx.x;
+    return KC ? t / 4 + THREADS / 4 * j : t / kAcross + THREADS / kAcross * j;
+  }
+  __device__ __forceinline__ int col_of() const {
+    const int t = threadIdx.x;
+    return E * (KC ? t % 4 : t % kAcross);
+  }
+
+  // The memory that holds k0 .. k0 + KT - 1.
+  struct Step {
+    __amdgpu_buffer_rsrc_t w;
+    int lines, limit;  // lines and columns inside
+  };
+  __device__ __forceinline__ Step step(int k0) const {
+    const int64_t skip = KC ? static_cast<int64_t>(k0) * kSrc : static_cast<int64_t>(k0) * ld;
+    const int left = depth - k0;
+    const int lines = KC ? rows : left < KT ? left : KT;
+    const int64_t bytes = (lines - 1) * ld + (KC ? left : rows) * static_cast<int64_t>(kSrc);
+    return Step{window(base + skip, lines > 0 && left > 0 ? bytes : 0), lines, KC ? left : rows};
+  }
+
+  // Chunk j of a step: into registers, then into LDS.
+  __device__ __forceinline__ void load(const Step& s, int j) {
+    const int col = col_of();
+    if constexpr (VEC) {
+      const uint32_t o = KC && col >= s.limit ? kNowhere : off[j];
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
+      for (int q = 0; q < kWords; q += 4) {
+        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s.w, o + 4 * q, 0, 0));
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t m = m0 + tm + p, n = n0 + tn + q;
-      if (m >= M || n >= N) continue;
-      if constexpr (PASS == kLinearWeight) {
-        float* g = a.grads + static_cast<int64_t>(i) * a.grad_ld + a.weight + m * N + n;
-        *g = a.accumulate ? *g + c[p][q] : c[p][q];
-      } else if constexpr (AT == GASLOC_BF16) {
-        static_cast<uint16_t*>(a.out)[(r0 + m) * a.out_ld + n] =
-            static_cast<uint16_t>(f32x2_to_bf16x2(c[p][q], 0.0f) & 0xffffu);
+        for (int e = 0; e < 4; ++e) words[j][q + e] = v[e];
+      }
+    } else {
+      const bool line = row_of(j) < s.lines;
+      uint32_t e[E];
+#pragma unroll
+      for (int q = 0; q < E; ++q) {
+        const uint32_t o = line && col + q < s.limit ? off[j] + q * kSrc : kNowhere;
+        if constexpr (ST == GASLOC_BF16)
+          e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(s.w, o, 0, 0));
+        else
+          e[q] = __builtin_amdgcn_raw_buffer_load_b32(s.w, o, 0, 0);
+      }
+#pragma unroll
+      for (int q = 0; q < kWords; ++q) words[j][q] = ST == GASLOC_BF16 ? e[2 * q] | e[2 * q + 1] << 16 : e[q];
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, int j) const {
+    u32x4 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      v[q] = ST == CT ? words[j][q < kWords ? q : 0]
+                      : f32x2_to_bf16x2(__uint_as_float(words[j][(2 * q) % kWords]),
+                                        __uint_as_float(words[j][(2 * q + 1) % kWords]));
+    *reinterpret_cast<u32x4*>(lds + row_of(j) * kStride + col_of() * kSize) = v;
+  }
+
+  // The fragment of rows row .. row + 15: lane l has row l % 16, elements E (l / 16) .. of the step's k.
+  __device__ __forceinline__ static u32x4 fragment(const char* lds, int row) {
+    const int l = lane_id(), i = l % 16, g = l / 16;
+    if constexpr (KC) {
+      return *reinterpret_cast<const u32x4*>(lds + (row + i) * kStride + g * 16);
+    } else if constexpr (CT == GASLOC_BF16) {
+      // 16 lanes read four rows of k, 16 columns each; lane i gets column i
+      s16x4 part[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const char* p = lds + (g * 8 + h * 4 + i / 4) * kStride + (row + i % 4 * 4) * 2;
+        part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(reinterpret_cast<uintptr_t>(p)));
+      }
+      const u32x2 lo = __builtin_bit_cast(u32x2, part[0]), hi = __builtin_bit_cast(u32x2, part[1]);
+      return u32x4{lo.x, lo.y, hi.x, hi.y};
+    } else {
+      u32x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        v[q] = *reinterpret_cast<const uint32_t*>(lds + (g * 4 + q) * kStride + (row + i) * 4);
+      return v;
+    }
+  }
+};
+
+template <int CT>
+__device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (CT == GASLOC_BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[q]), __uint_as_float(b[q]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// A tile of TM x TN outputs by WAVES_M x WAVES_N waves.
+template <int PASS, int PT, int AT, int TM, int TN, int WAVES_M, int WAVES_N, bool VEC>
+__global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a) {
+  constexpr int THREADS = kWave * WAVES_M * WAVES_N;
+  constexpr bool kForward = PASS == kLinearForward, kWeight = PASS == kLinearWeight;
+  using OpA = Operand<TM, THREADS, !kWeight, AT, AT, VEC>;
+  using OpB = Operand<TN, THREADS, kForward, kWeight ? AT : PT, AT, VEC>;
+  constexpr int KT = OpA::KT;
+  constexpr int WM = TM / WAVES_M, WN = TN / WAVES_N, FM = WM / 16, FN = WN / 16;
+  __shared__ __align__(16) char s_tiles[kBuffers * (OpA::kLds + OpB::kLds)];
+  const auto s_a = [&](int k) { return s_tiles + k * OpA::kLds; };
+  const auto s_b = [&](int k) { return s_tiles + kBuffers * OpA::kLds + k * OpB::kLds; };
+
+  // Workgroups go round the eight XCDs: each gets a contiguous stretch of the tiles, which share rows of A or B in
+  // its L2.
+  const int total = a.tiles.begin[a.n], b = blockIdx.x;
+  const int each = total / 8, more = total % 8, xcd = b % 8;
+  const int t = xcd * each + (xcd < more ? xcd : more) + b / 8;
+  const int i = find_worker(a.tiles, a.n, t);
+  const int tile = t - a.tiles.begin[i];
+  const int64_t r0 = a.rows.begin[i];
+  const int count = a.rows.begin[i + 1] - a.rows.begin[i];
+  const int M = kWeight ? a.out_features : count;
+  const int N = kForward ? a.out_features : a.in_features;
+  const int depth = kForward ? a.in_features : kWeight ? count : a.out_features;
+  const int across = (N + TN - 1) / TN;
+  const int m0 = tile / across * TM, n0 = tile % across * TN;
+  constexpr int kAct = AT == GASLOC_BF16 ? 2 : 4, kPar = PT == GASLOC_BF16 ? 2 : 4;
+  const char* w = static_cast<const char*>(live_row<PT>(a.w, i)) + a.weight * kPar;
+
+  OpA oa;
+  OpB ob;
+  if constexpr (kForward) {
+    oa.start(static_cast<const char*>(a.x) + (r0 + m0) * a.x_ld * kAct, a.x_ld, M - m0, depth);
+    ob.start(w + static_cast<int64_t>(n0) * depth * kPar, depth, N - n0, depth);
+  } else if constexpr (!kWeight) {
+    oa.start(static_cast<const char*>(a.dout) + (r0 + m0) * a.dout_ld * kAct, a.dout_ld, M - m0, depth);
+    ob.start(w + static_cast<int64_t>(n0) * kPar, N, N - n0, depth);
+  } else {
+    oa.start(static_cast<const char*>(a.dout) + (r0 * a.dout_ld + m0) * kAct, a.dout_ld, M - m0, depth);
+    ob.start(static_cast<const char*>(a.x) + (r0 * a.x_ld + n0) * kAct, a.x_ld, N - n0, depth);
+  }
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
+  f32x4 c[FM][FN];
+#pragma unroll
+  for (int p = 0; p < FM; ++p) {
+#pragma unroll
+    for (int q = 0; q < FN; ++q) c[p][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  if (depth > 0) {
+    // In step k its fragments are multiplied, those of step k + 1 are read from the next buffer, step k + 2 is
+    // stored into the one after it, and step k + 3 is loaded: all of it in between the rows of products, so that
+    // the matrix cores do not wait for any of it.
+    constexpr int CA = OpA::kChunks, CB = OpB::kChunks;
+#pragma unroll
+    for (int k = 0; k < kBuffers; ++k) {
+      const auto la = oa.step(k * KT);
+      const auto lb = ob.step(k * KT);
+#pragma unroll
+      for (int j = 0; j < CA; ++j) oa.load(la, j);
+#pragma unroll
+      for (int j = 0; j < CB; ++j) ob.load(lb, j);
+      if (k == kBuffers - 1) break;
+#pragma unroll
+      for (int j = 0; j < CA; ++j) oa.store(s_a(k), j);
+#pragma unroll
+      for (int j = 0; j < CB; ++j) ob.store(s_b(k), j);
+    }
+    __syncthreads();
+    int cur = 0;
+    u32x4 fa[4], fb[2][FN];  // A's fragments are read four rows ahead
+    static_assert(FM % 4 == 0, "the rows go round the fragments evenly");
+#pragma unroll
+    for (int p = 0; p < 4; ++p) fa[p] = OpA::fragment(s_a(0), wm + 16 * p);
+#pragma unroll
+    for (int q = 0; q < FN; ++q) fb[0][q] = OpB::fragment(s_b(0), wn + 16 * q);
+    const auto one_step = [&](int k0, const u32x4(&now)[FN], u32x4(&then)[FN]) {
+      const int next = cur == kBuffers - 1 ? 0 : cur + 1, free = next == kBuffers - 1 ? 0 : next + 1;
+      const auto la = oa.step(k0 + 3 * KT);
+      const auto lb = ob.step(k0 + 3 * KT);
+#pragma unroll
+      for (int p = 0; p < FM; ++p) {
+        // behind the last step, too, where loads give zeros: there is no branch in the loop
+#pragma unroll
+        for (int j = p * (CA + CB) / FM; j < (p + 1) * (CA + CB) / FM; ++j) {
+          if (j < CA) {
+            oa.store(s_a(free), j);
+            oa.load(la, j);
+          } else {
+            ob.store(s_b(free), j - CA);
+            ob.load(lb, j - CA);
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < FN; ++q) c[p][q] = multiply<AT>(now[q], fa[p % 4], c[p][q]);  // lane: row l % 16 of C
+        fa[p % 4] = p + 4 < FM ? OpA::fragment(s_a(cur), wm + 16 * (p + 4))
+                               : OpA::fragment(s_a(next), wm + 16 * (p + 4 - FM));
+#pragma unroll
+        for (int q = p * FN / FM; q < (p + 1) * FN / FM; ++q) then[q] = OpB::fragment(s_b(next), wn + 16 * q);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __syncthreads();
+      cur = next;
+    };
+#pragma unroll 1
+    for (int k0 = 0; k0 < depth; k0 += 2 * KT) {  // the second of the two may be all zeros
+      one_step(k0, fb[0], fb[1]);
+      one_step(k0 + KT, fb[1], fb[0]);
+    }
+  }
+
+  // Lane l holds row l % 16 and columns 4 (l / 16) .. + 3 of each 16 x 16 block.  Sixteen rows at a time go
+  // through the wave's own part of LDS, so that whole lines are stored.
+  using Out = typename std::conditional<kWeight || AT == GASLOC_F32, float, uint16_t>::type;
+  constexpr int kOutStride = WN * static_cast<int>(sizeof(Out)) + 16;
+  constexpr int V = VEC ? 16 / static_cast<int>(sizeof(Out)) : 1;
+  static_assert(THREADS / kWave * 16 * kOutStride <= kBuffers * (OpA::kLds + OpB::kLds), "sixteen rows of every wave fit");
+  char* const mine = s_tiles + wave * 16 * kOutStride;
+  const int lane = lane_id();
+  Out* const out = kWeight ? reinterpret_cast<Out*>(a.grads + static_cast<int64_t>(i) * a.grad_ld + a.weight)
+                           : static_cast<Out*>(a.out) + r0 * a.out_ld;
+  const int64_t out_ld = kWeight ? N : a.out_ld;
+#pragma unroll
+  for (int p = 0; p < FM; ++p) {
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < FN; ++q) {
+      char* to = mine + lane % 16 * kOutStride + (16 * q + lane / 16 * 4) * static_cast<int>(sizeof(Out));
+      if constexpr (sizeof(Out) == 4)
+        *reinterpret_cast<f32x4*>(to) = c[p][q];
+      else
+        *reinterpret_cast<u32x2*>(to) =
+            u32x2{f32x2_to_bf16x2(c[p][q][0], c[p][q][1]), f32x2_to_bf16x2(c[p][q][2], c[p][q][3])};
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int top = m0 + wm + 16 * p;
+#pragma unroll 4
+    for (int e = lane * V; e < 16 * WN; e += kWave * V) {
+      const int row = e / WN, col = e % WN, n = n0 + wn + col;
+      if (top + row >= M || n >= N) continue;
+      const char* from = mine + row * kOutStride + col * static_cast<int>(sizeof(Out));
+      Out* to = out + (top + row) * out_ld + n;
+      if constexpr (VEC && kWeight) {
+        f32x4 v = *reinterpret_cast<const f32x4*>(from);
+        if (a.accumulate) v += *reinterpret_cast<const f32x4*>(to);
+        *reinterpret_cast<f32x4*>(to) = v;
+      } else if constexpr (VEC) {
+        *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(from);
       } else {
-        static_cast<float*>(a.out)[(r0 + m) * a.out_ld + n] = c[p][q];
+        const Out v = *reinterpret_cast<const Out*>(from);
+        if constexpr (kWeight)
+          *to = a.accumulate ? *to + v : v;
+        else
+          *to = v;
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
+}
+
+template <int PASS, int PT, int AT>
+hipError_t launch_types(const LinearArgs& a, int tile, bool vec, hipStream_t stream) {
+  const dim3 grid(a.tiles.begin[a.n]);
+  if constexpr (AT == GASLOC_BF16) {
+    if (tile == 256) return launch_kernel(k_linear<PASS, PT, AT, 256, 256, 2, 4, true>, grid, 512, 0, stream, a);
+  }
+  return launch_kernel(vec ? k_linear<PASS, PT, AT, 128, 128, 2, 2, true> : k_linear<PASS, PT, AT, 128, 128, 2, 2, false>,
+                       grid, 256, 0, stream, a);
 }
 
 template <int PASS>
-hipError_t launch(const LinearArgs& a, int params, int act, hipStream_t stream) {
-  return launch_kernel(params == GASLOC_BF16 ? k_linear<PASS, GASLOC_BF16, GASLOC_BF16>
-                       : act == GASLOC_BF16  ? k_linear<PASS, GASLOC_F32, GASLOC_BF16>
-                                             : k_linear<PASS, GASLOC_F32, GASLOC_F32>,
-                       dim3(a.tiles.begin[a.n]), 256, 0, stream, a);
+hipError_t launch(const LinearArgs& a, int params, int act, int tile, bool vec, hipStream_t stream) {
+  // the weight's gradient does not read the parameters
+  if (PASS != kLinearWeight && params == GASLOC_BF16)
+    return launch_types<PASS, PASS == kLinearWeight ? GASLOC_F32 : GASLOC_BF16, GASLOC_BF16>(a, tile, vec, stream);
+  if (act == GASLOC_BF16) return launch_types<PASS, GASLOC_F32, GASLOC_BF16>(a, tile, vec, stream);
+  return launch_types<PASS, GASLOC_F32, GASLOC_F32>(a, tile, vec, stream);
 }
 
 }  // namespace
 
-hipError_t launch_linear(const LinearArgs& a, LinearPass pass, int params, int act, hipStream_t stream) {
-  if (pass == kLinearForward) return launch<kLinearForward>(a, params, act, stream);
-  if (pass == kLinearInput) return launch<kLinearInput>(a, params, act, stream);
-  return launch<kLinearWeight>(a, params, act, stream);
+hipError_t launch_linear(const LinearArgs& a, LinearPass pass, int params, int act, int tile, bool vec,
+                         hipStream_t stream) {
+  if (pass == kLinearForward) return launch<kLinearForward>(a, params, act, tile, vec, stream);
+  if (pass == kLinearInput) return launch<kLinearInput>(a, params, act, tile, vec, stream);
+  return launch<kLinearWeight>(a, params, act, tile, vec, stream);
 }
 
 }  // namespace gasloc
