@@ -206,19 +206,24 @@ std::string check_weight(const gasloc_ctx& c, int64_t weight, int32_t out_featur
   return check_columns(c, "weight", weight, static_cast<int64_t>(out_features) * in_features);
 }
 
-// Tiles of every worker's product; false if there are too many for one launch.
-bool linear_tiles(int n, const int64_t* row_ptr, const gasloc::LinearArgs& a, gasloc::LinearPass pass, int tile,
-                  Spans* tiles) {
+// Tiles of every worker's product; false if there are too many for one launch.  The weight's gradient begins with
+// the workers that have the most rows, whose tiles take longest.
+bool linear_tiles(int n, const int64_t* row_ptr, gasloc::LinearPass pass, int tile, gasloc::LinearArgs* a) {
   const auto cut = [tile](int64_t v) { return (v + tile - 1) / tile; };
+  for (int i = 0; i < n; ++i) a->order[i] = static_cast<uint8_t>(i);
+  if (pass == gasloc::kLinearWeight)
+    std::stable_sort(a->order, a->order + n, [&](int i, int j) {
+      return row_ptr[i + 1] - row_ptr[i] > row_ptr[j + 1] - row_ptr[j];
+    });
   int64_t at = 0;
-  tiles->begin[0] = 0;
+  a->tiles.begin[0] = 0;
   for (int i = 0; i < n; ++i) {
     const int64_t rows = row_ptr[i + 1] - row_ptr[i];
-    at += pass == gasloc::kLinearWeight    ? cut(a.out_features) * cut(a.in_features)
-          : pass == gasloc::kLinearForward ? cut(rows) * cut(a.out_features)
-                                           : cut(rows) * cut(a.in_features);
+    at += pass == gasloc::kLinearWeight    ? cut(a->out_features) * cut(a->in_features)
+          : pass == gasloc::kLinearForward ? cut(rows) * cut(a->out_features)
+                                           : cut(rows) * cut(a->in_features);
     if (at > INT_MAX) return false;
-    tiles->begin[i + 1] = static_cast<int32_t>(at);
+    a->tiles.begin[i + 1] = static_cast<int32_t>(at);
   }
   return true;
 }
@@ -233,10 +238,10 @@ gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPas
                    (!a->out || vector_rows(a->out, a->out_ld, 0, dtype)) && a->in_features % 8 == 0 &&
                    a->out_features % 8 == 0;
   int tile = vec && dtype == GASLOC_BF16 ? 256 : 128;
-  bool fits = linear_tiles(c->n, row_ptr, *a, pass, tile, &a->tiles);
+  bool fits = linear_tiles(c->n, row_ptr, pass, tile, a);
   if (fits && tile == 256 && a->tiles.begin[c->n] < 2 * c->cus) {
     tile = 128;
-    fits = linear_tiles(c->n, row_ptr, *a, pass, tile, &a->tiles);
+    fits = linear_tiles(c->n, row_ptr, pass, tile, a);
   }
   if (!fits) return fail(c, GASLOC_EINVAL, "product too large for one launch");
   if (a->tiles.begin[c->n] == 0) return GASLOC_OK;

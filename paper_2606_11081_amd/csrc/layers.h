@@ -146,6 +146,7 @@ struct LinearArgs {
   int64_t grad_ld;
   int32_t accumulate;
   Spans rows, tiles;
+  uint8_t order[kMaxReplicas];  // weight: the worker of each span of tiles
 };
 // tile: rows and columns of a workgroup's part of C (256, or 128: always 128 without vec and in F32); vec: every row of either operand, of C and of
 // the gradients begins on a 16-byte boundary and is a whole number of 16-byte chunks of activations.

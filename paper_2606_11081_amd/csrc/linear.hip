@@ -21,51 +21,65 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kRowBytes = 80;   // a [row][k] row in LDS: 64 bytes and 16 that spread the rows over the banks
-constexpr int kBuffers = 3;
+constexpr int kBuffers = 4;
 constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset no buffer holds: the load gives zeros
 
 // A range of memory that loads are checked against; what lies outside reads as zero.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* p, int64_t bytes) {
-  const uint32_t n = bytes <= 0 ? 0u : bytes > 0x80000000ll ? 0x80000000u : static_cast<uint32_t>(bytes);
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(n), 0x00027000);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(bytes), 0x00027000);
 }
 
-// One operand of a workgroup's tile: ROWS rows (of m or n), KT of k at a time.
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* lds_pointer(uint32_t at) {
+  return (__attribute__((address_space(3))) T*)static_cast<uintptr_t>(at);
+}
+
+// One operand of a workgroup's tile: ROWS rows (of m or n), KT of k per step.
 // KC: rows run along k in memory.  ST: type in memory, CT: type of the product.
 // VEC: 16-byte chunks lie on 16-byte boundaries and are inside or outside as a whole.
+//
+// In LDS a KC step is [row][64 bytes], its four chunks permuted by the row's
+// place among sixteen; other bf16 steps are [k][row], blocks of 32 bytes
+// permuted by k; fp32 ones have their lines 16 bytes apart.  So neither the
+// writes nor the lanes that a fragment read serves at a time meet in a bank
+// (plain padding of 16 bytes per KC row cost as many cycles in conflicts again).
 template <int ROWS, int THREADS, bool KC, int ST, int CT, bool VEC>
 struct Operand {
-  static constexpr int kSize = CT == GASLOC_BF16 ? 2 : 4;        // bytes of an element in LDS
-  static constexpr int kSrc = ST == GASLOC_BF16 ? 2 : 4;         // and in memory
-  static constexpr int E = 16 / kSize;                           // elements of a chunk in LDS
-  static constexpr int KT = 4 * E;                               // k per step
-  static constexpr int kChunks = ROWS * 4 / THREADS;      // chunks per thread
-  static constexpr int kWords = E * kSrc / 4;                    // words of a chunk in memory
-  static constexpr int kAcross = ROWS / E;                       // chunks of a [k][row] row
-  static constexpr int kStride = KC ? kRowBytes : ROWS * kSize + (CT == GASLOC_BF16 ? 32 : 16);
+  static constexpr int kSize = CT == GASLOC_BF16 ? 2 : 4;  // bytes of an element in LDS
+  static constexpr int kSrc = ST == GASLOC_BF16 ? 2 : 4;   // and in memory
+  static constexpr int E = 16 / kSize;                     // elements of a chunk in LDS
+  static constexpr int KT = 4 * E;                         // k per step
+  static constexpr int kChunks = ROWS * 4 / THREADS;       // chunks per thread
+  static constexpr int kWords = E * kSrc / 4;              // words of a chunk in memory
+  static constexpr int kAcross = ROWS / E;                 // chunks of a [k][row] line
+  static constexpr int kStride = KC ? 64 : ROWS * kSize + (CT == GASLOC_BF16 ? 0 : 16);
   static constexpr int kLds = KC ? ROWS * kStride : KT * kStride;
 
-  const char* base;   // row 0, k 0 of the tile
-  int64_t ld;         // bytes between rows in memory
-  int rows, depth;    // rows inside (of ROWS), length of k
+  const char* at;  // row 0 of the step to be loaded next
+  int left;        // k from there on
+  int64_t ahead;   // bytes to the next step
+  uint32_t line;   // bytes between lines in memory
+  int rows;        // rows inside (of ROWS)
+  uint32_t full;   // bytes of a whole step (not KC) or of the rows from `at` on (KC)
   uint32_t off[kChunks];
-  uint32_t words[kChunks][kWords];
+  typedef uint32_t Words[kChunks][kWords];  // a step on its way to LDS
 
-  // p: element (first, 0) of the operand; `rows` rows from there on exist
-  __device__ __forceinline__ void start(const void* p, int64_t ld_elements, int64_t rows_left, int64_t k) {
-    base = static_cast<const char*>(p);
-    ld = ld_elements * kSrc;
-    rows = static_cast<int>(rows_left < ROWS ? rows_left : ROWS);
-    depth = static_cast<int>(k);
+  // p: element (first, 0) of the operand; `rows_left` rows from there on exist
+  __device__ __forceinline__ void start(const void* p, int64_t ld, int rows_left, int k) {
+    at = static_cast<const char*>(p);
+    line = static_cast<uint32_t>(ld * kSrc);
+    rows = rows_left < ROWS ? rows_left : ROWS;
+    left = k;
+    ahead = KC ? KT * kSrc : KT * static_cast<int64_t>(line);
+    full = KC ? static_cast<uint32_t>(rows - 1) * line + static_cast<uint32_t>(k) * kSrc
+              : static_cast<uint32_t>(KT - 1) * line + static_cast<uint32_t>(rows) * kSrc;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) {
-      const int row = row_of(j), col = col_of();
-      off[j] = static_cast<uint32_t>(row * ld + col * kSrc);
-      if (!KC && VEC && col >= rows) off[j] = kNowhere;
+      off[j] = static_cast<uint32_t>(row_of(j)) * line + static_cast<uint32_t>(col_of() * kSrc);
+      if (!KC && VEC && col_of() >= rows) off[j] = kNowhere;
     }
   }
-  // The chunk j of this thread: its row in memory (of m or n, or of k) and its first column.
+  // The chunk j of this thread: its line in memory (a row of m or n, or of k) and its first column.
   __device__ __forceinline__ int row_of(int j) const {
     const int t = threadIdx.x;
     return KC ? t / 4 + THREADS / 4 * j : t / kAcross + THREADS / kAcross * j;
@@ -75,21 +89,23 @@ struct Operand {
     return E * (KC ? t % 4 : t % kAcross);
   }
 
-  // The memory that holds k0 .. k0 + KT - 1.
   struct Step {
     __amdgpu_buffer_rsrc_t w;
     int lines, limit;  // lines and columns inside
   };
-  __device__ __forceinline__ Step step(int k0) const {
-    const int64_t skip = KC ? static_cast<int64_t>(k0) * kSrc : static_cast<int64_t>(k0) * ld;
-    const int left = depth - k0;
-    const int lines = KC ? rows : left < KT ? left : KT;
-    const int64_t bytes = (lines - 1) * ld + (KC ? left : rows) * static_cast<int64_t>(kSrc);
-    return Step{window(base + skip, lines > 0 && left > 0 ? bytes : 0), lines, KC ? left : rows};
+  // The memory of the next step; `at` moves on.  Behind the last step nothing is inside.
+  __device__ __forceinline__ Step next() {
+    const int inside = left < 0 ? 0 : left < KT ? left : KT;
+    const uint32_t bytes = KC ? full : full - static_cast<uint32_t>(KT - inside) * line;
+    const Step s{window(at, left > 0 ? bytes : 0), KC ? rows : inside, KC ? left : rows};
+    if (KC) full -= KT * kSrc;
+    at += ahead;
+    left -= KT;
+    return s;
   }
 
   // Chunk j of a step: into registers, then into LDS.
-  __device__ __forceinline__ void load(const Step& s, int j) {
+  __device__ __forceinline__ void load(const Step& s, int j, Words& words) const {
     const int col = col_of();
     if constexpr (VEC) {
       const uint32_t o = KC && col >= s.limit ? kNowhere : off[j];
@@ -100,11 +116,11 @@ struct Operand {
         for (int e = 0; e < 4; ++e) words[j][q + e] = v[e];
       }
     } else {
-      const bool line = row_of(j) < s.lines;
+      const bool inside = row_of(j) < s.lines;
       uint32_t e[E];
 #pragma unroll
       for (int q = 0; q < E; ++q) {
-        const uint32_t o = line && col + q < s.limit ? off[j] + q * kSrc : kNowhere;
+        const uint32_t o = inside && col + q < s.limit ? off[j] + q * kSrc : kNowhere;
         if constexpr (ST == GASLOC_BF16)
           e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(s.w, o, 0, 0));
         else
@@ -114,37 +130,55 @@ struct Operand {
       for (int q = 0; q < kWords; ++q) words[j][q] = ST == GASLOC_BF16 ? e[2 * q] | e[2 * q + 1] << 16 : e[q];
     }
   }
-  __device__ __forceinline__ void store(char* lds, int j) const {
+  // LDS addresses: where chunk 0 of this thread goes (chunk j lies kChunkStep further on), and the lane's part of the
+  // fragment that begins at row `row` of the tile.
+  static constexpr int kChunkStep = (KC ? THREADS / 4 : THREADS / kAcross) * kStride;
+  __device__ __forceinline__ uint32_t store_at(uint32_t lds) const {
+    const int row = row_of(0), chunk = col_of() / E;
+    const int to = KC                     ? (chunk ^ (0 - row / 4 & 3)) * 16
+                   : CT == GASLOC_BF16 ? ((chunk / 2 ^ across(row)) * 2 + chunk % 2) * 16
+                                       : chunk * 16;
+    return lds + row * kStride + to;
+  }
+  __device__ __forceinline__ static uint32_t read_at(uint32_t lds, int row) {
+    const int l = lane_id(), i = l % 16, g = l / 16;
+    if constexpr (KC)
+      return lds + (row + i) * kStride + (g ^ (0 - i / 4 & 3)) * 16;
+    else if constexpr (CT == GASLOC_BF16)
+      return lds + (g * 8 + i / 4) * kStride + (row / 16 ^ across(g * 8 + i / 4)) * 32 + i % 4 * 8;
+    else
+      return lds + g * 4 * kStride + (row + i) * 4;
+  }
+  // How the 32-byte blocks of line k are permuted.
+  __device__ __forceinline__ static int across(int k) { return k % 4 + k / 8 % 2 * 4; }
+
+  __device__ __forceinline__ void store(uint32_t to, int j, const Words& words) const {
+    static_assert(KC || CT != GASLOC_BF16 || THREADS / kAcross % 16 == 0 || kChunks == 1,
+                  "the chunks of a thread are permuted alike");
     u32x4 v;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       v[q] = ST == CT ? words[j][q < kWords ? q : 0]
                       : f32x2_to_bf16x2(__uint_as_float(words[j][(2 * q) % kWords]),
                                         __uint_as_float(words[j][(2 * q + 1) % kWords]));
-    *reinterpret_cast<u32x4*>(lds + row_of(j) * kStride + col_of() * kSize) = v;
+    *lds_pointer<u32x4>(to + j * kChunkStep) = v;
   }
-
-  // The fragment of rows row .. row + 15: lane l has row l % 16, elements E (l / 16) .. of the step's k.
-  __device__ __forceinline__ static u32x4 fragment(const char* lds, int row) {
-    const int l = lane_id(), i = l % 16, g = l / 16;
+  // The fragment of sixteen rows, the p-th from the row `from` was made for: lane l has row l % 16, elements
+  // E (l / 16) .. of the step's k.  `buffer`: how far the step's buffer lies behind the first.
+  __device__ __forceinline__ static u32x4 fragment(uint32_t from, int buffer, int p) {
     if constexpr (KC) {
-      return *reinterpret_cast<const u32x4*>(lds + (row + i) * kStride + g * 16);
+      return *lds_pointer<const u32x4>(from + buffer + p * 16 * kStride);
     } else if constexpr (CT == GASLOC_BF16) {
-      // 16 lanes read four rows of k, 16 columns each; lane i gets column i
-      s16x4 part[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const char* p = lds + (g * 8 + h * 4 + i / 4) * kStride + (row + i % 4 * 4) * 2;
-        part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(reinterpret_cast<uintptr_t>(p)));
-      }
-      const u32x2 lo = __builtin_bit_cast(u32x2, part[0]), hi = __builtin_bit_cast(u32x2, part[1]);
+      // 16 lanes read four lines of k, 16 columns each; lane i gets column i
+      const uint32_t at = (from ^ p % 8 * 32) + p / 8 * 256 + buffer;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_pointer<s16x4>(at)));
+      const u32x2 hi =
+          __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_pointer<s16x4>(at + 4 * kStride)));
       return u32x4{lo.x, lo.y, hi.x, hi.y};
     } else {
       u32x4 v;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        v[q] = *reinterpret_cast<const uint32_t*>(lds + (g * 4 + q) * kStride + (row + i) * 4);
+      for (int q = 0; q < 4; ++q) v[q] = *lds_pointer<const uint32_t>(from + buffer + q * kStride + p * 64);
       return v;
     }
   }
@@ -173,16 +207,22 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   constexpr int KT = OpA::KT;
   constexpr int WM = TM / WAVES_M, WN = TN / WAVES_N, FM = WM / 16, FN = WN / 16;
   __shared__ __align__(16) char s_tiles[kBuffers * (OpA::kLds + OpB::kLds)];
-  const auto s_a = [&](int k) { return s_tiles + k * OpA::kLds; };
-  const auto s_b = [&](int k) { return s_tiles + kBuffers * OpA::kLds + k * OpB::kLds; };
+  const uint32_t lds_a = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)s_tiles));
+  const uint32_t lds_b = lds_a + kBuffers * OpA::kLds;
 
-  // Workgroups go round the eight XCDs: each gets a contiguous stretch of the tiles, which share rows of A or B in
-  // its L2.
-  const int total = a.tiles.begin[a.n], b = blockIdx.x;
-  const int each = total / 8, more = total % 8, xcd = b % 8;
-  const int t = xcd * each + (xcd < more ? xcd : more) + b / 8;
-  const int i = find_worker(a.tiles, a.n, t);
-  const int tile = t - a.tiles.begin[i];
+  // Workgroups go round the eight XCDs.  Each XCD gets a contiguous stretch of tiles, which share rows of A or B in
+  // its L2: of all the tiles, where tiles cost the same; of every worker's tiles in the weight's gradient, whose
+  // cost is the worker's number of rows (the workers with the most rows come first, in `order`).
+  const int b = blockIdx.x;
+  const int owner = kWeight ? find_worker(a.tiles, a.n, b) : 0;
+  const int from = kWeight ? a.tiles.begin[owner] : 0;
+  const int total = a.tiles.begin[kWeight ? owner + 1 : a.n] - from;
+  const int xcd = (b - from) % 8, each = total / 8, more = total % 8;
+  const int t = from + xcd * each + (xcd < more ? xcd : more) + (b - from) / 8;
+  const int span = kWeight ? owner : find_worker(a.tiles, a.n, t);
+  const int i = kWeight ? a.order[span] : span;
+  const int tile = t - a.tiles.begin[span];
   const int64_t r0 = a.rows.begin[i];
   const int count = a.rows.begin[i + 1] - a.rows.begin[i];
   const int M = kWeight ? a.out_features : count;
@@ -218,62 +258,74 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   if (depth > 0) {
     // In step k its fragments are multiplied, those of step k + 1 are read from the next buffer, step k + 2 is
     // stored into the one after it, and step k + 3 is loaded: all of it in between the rows of products, so that
-    // the matrix cores do not wait for any of it.
+    // the matrix cores do not wait for any of it.  Behind the last step loads give zeros: there is no branch in the
+    // loop.
     constexpr int CA = OpA::kChunks, CB = OpB::kChunks;
+    const uint32_t put_a = oa.store_at(lds_a), put_b = ob.store_at(lds_b);
+    const uint32_t get_a = OpA::read_at(lds_a, wm), get_b = OpB::read_at(lds_b, wn);
+    typename OpA::Words wa;
+    typename OpB::Words wb;
+    {
+      typename OpA::Words wa0, wa1;
+      typename OpB::Words wb0, wb1;
+      const auto load_step = [&](typename OpA::Words& to_a, typename OpB::Words& to_b) {
+        const auto la = oa.next();
+        const auto lb = ob.next();
 #pragma unroll
-    for (int k = 0; k < kBuffers; ++k) {
-      const auto la = oa.step(k * KT);
-      const auto lb = ob.step(k * KT);
+        for (int j = 0; j < CA; ++j) oa.load(la, j, to_a);
 #pragma unroll
-      for (int j = 0; j < CA; ++j) oa.load(la, j);
+        for (int j = 0; j < CB; ++j) ob.load(lb, j, to_b);
+      };
+      load_step(wa0, wb0);
+      load_step(wa1, wb1);
+      load_step(wa, wb);
 #pragma unroll
-      for (int j = 0; j < CB; ++j) ob.load(lb, j);
-      if (k == kBuffers - 1) break;
+      for (int j = 0; j < CA; ++j) oa.store(put_a, j, wa0);
 #pragma unroll
-      for (int j = 0; j < CA; ++j) oa.store(s_a(k), j);
+      for (int j = 0; j < CB; ++j) ob.store(put_b, j, wb0);
 #pragma unroll
-      for (int j = 0; j < CB; ++j) ob.store(s_b(k), j);
+      for (int j = 0; j < CA; ++j) oa.store(put_a + OpA::kLds, j, wa1);
+#pragma unroll
+      for (int j = 0; j < CB; ++j) ob.store(put_b + OpB::kLds, j, wb1);
     }
     __syncthreads();
-    int cur = 0;
     u32x4 fa[4], fb[2][FN];  // A's fragments are read four rows ahead
     static_assert(FM % 4 == 0, "the rows go round the fragments evenly");
 #pragma unroll
-    for (int p = 0; p < 4; ++p) fa[p] = OpA::fragment(s_a(0), wm + 16 * p);
+    for (int p = 0; p < 4; ++p) fa[p] = OpA::fragment(get_a, 0, p);
 #pragma unroll
-    for (int q = 0; q < FN; ++q) fb[0][q] = OpB::fragment(s_b(0), wn + 16 * q);
-    const auto one_step = [&](int k0, const u32x4(&now)[FN], u32x4(&then)[FN]) {
-      const int next = cur == kBuffers - 1 ? 0 : cur + 1, free = next == kBuffers - 1 ? 0 : next + 1;
-      const auto la = oa.step(k0 + 3 * KT);
-      const auto lb = ob.step(k0 + 3 * KT);
-#pragma unroll
-      for (int p = 0; p < FM; ++p) {
-        // behind the last step, too, where loads give zeros: there is no branch in the loop
-#pragma unroll
-        for (int j = p * (CA + CB) / FM; j < (p + 1) * (CA + CB) / FM; ++j) {
-          if (j < CA) {
-            oa.store(s_a(free), j);
-            oa.load(la, j);
-          } else {
-            ob.store(s_b(free), j - CA);
-            ob.load(lb, j - CA);
-          }
-        }
-#pragma unroll
-        for (int q = 0; q < FN; ++q) c[p][q] = multiply<AT>(now[q], fa[p % 4], c[p][q]);  // lane: row l % 16 of C
-        fa[p % 4] = p + 4 < FM ? OpA::fragment(s_a(cur), wm + 16 * (p + 4))
-                               : OpA::fragment(s_a(next), wm + 16 * (p + 4 - FM));
-#pragma unroll
-        for (int q = p * FN / FM; q < (p + 1) * FN / FM; ++q) then[q] = OpB::fragment(s_b(next), wn + 16 * q);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      __syncthreads();
-      cur = next;
-    };
+    for (int q = 0; q < FN; ++q) fb[0][q] = OpB::fragment(get_b, 0, q);
 #pragma unroll 1
-    for (int k0 = 0; k0 < depth; k0 += 2 * KT) {  // the second of the two may be all zeros
-      one_step(k0, fb[0], fb[1]);
-      one_step(k0 + KT, fb[1], fb[0]);
+    for (int k0 = 0; k0 < depth; k0 += kBuffers * KT) {
+#pragma unroll
+      for (int cur = 0; cur < kBuffers; ++cur) {
+        constexpr int kMask = kBuffers - 1;
+        const int next = cur + 1 & kMask, free = cur + 2 & kMask, h = cur & 1;
+        const auto la = oa.next();
+        const auto lb = ob.next();
+#pragma unroll
+        for (int p = 0; p < FM; ++p) {
+#pragma unroll
+          for (int q = 0; q < FN; ++q) c[p][q] = multiply<AT>(fb[h][q], fa[p % 4], c[p][q]);  // lane: row l % 16 of C
+          fa[p % 4] = p + 4 < FM ? OpA::fragment(get_a, cur * OpA::kLds, p + 4)
+                                 : OpA::fragment(get_a, next * OpA::kLds, p + 4 - FM);
+#pragma unroll
+          for (int q = p * FN / FM; q < (p + 1) * FN / FM; ++q)
+            fb[h ^ 1][q] = OpB::fragment(get_b, next * OpB::kLds, q);
+#pragma unroll
+          for (int j = p * (CA + CB) / FM; j < (p + 1) * (CA + CB) / FM; ++j) {
+            if (j < CA) {
+              oa.store(put_a + free * OpA::kLds, j, wa);
+              oa.load(la, j, wa);
+            } else {
+              ob.store(put_b + free * OpB::kLds, j - CA, wb);
+              ob.load(lb, j - CA, wb);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+      }
     }
   }
 
