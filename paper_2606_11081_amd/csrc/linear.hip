@@ -29,6 +29,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* p, uint32_t
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(bytes), 0x00027000);
 }
 
+// All waves meet; of this wave's LDS operations all but the last READS are done.
+template <int READS>
+__device__ __forceinline__ void step_barrier() {
+  static_assert(READS < 16, "the counter's range");
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" : : "n"(READS) : "memory");
+}
+
 template <typename T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_pointer(uint32_t at) {
   return (__attribute__((address_space(3))) T*)static_cast<uintptr_t>(at);
@@ -45,6 +53,7 @@ __device__ __forceinline__ __attribute__((address_space(3))) T* lds_pointer(uint
 // (plain padding of 16 bytes per KC row cost as many cycles in conflicts again).
 template <int ROWS, int THREADS, bool KC, int ST, int CT, bool VEC>
 struct Operand {
+  static constexpr bool kColumns = KC;
   static constexpr int kSize = CT == GASLOC_BF16 ? 2 : 4;  // bytes of an element in LDS
   static constexpr int kSrc = ST == GASLOC_BF16 ? 2 : 4;   // and in memory
   static constexpr int E = 16 / kSize;                     // elements of a chunk in LDS
@@ -229,7 +238,12 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   const int N = kForward ? a.out_features : a.in_features;
   const int depth = kForward ? a.in_features : kWeight ? count : a.out_features;
   const int across = (N + TN - 1) / TN;
-  const int m0 = tile / across * TM, n0 = tile % across * TN;
+  // kGroup tiles of m by all of n at a time, m first: the tiles that an XCD works on at once are about as many of m as
+  // of n, which is what has to be read least for.
+  constexpr int kGroup = TM == 256 ? 4 : 8;
+  const int group = tile / (kGroup * across), in_group = tile % (kGroup * across);
+  const int tall = min(kGroup, (M + TM - 1) / TM - group * kGroup);
+  const int m0 = (group * kGroup + in_group % tall) * TM, n0 = in_group / tall * TN;
   constexpr int kAct = AT == GASLOC_BF16 ? 2 : 4, kPar = PT == GASLOC_BF16 ? 2 : 4;
   const char* w = static_cast<const char*>(live_row<PT>(a.w, i)) + a.weight * kPar;
 
@@ -291,6 +305,11 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
     __syncthreads();
     u32x4 fa[4], fb[2][FN];  // A's fragments are read four rows ahead
     static_assert(FM % 4 == 0, "the rows go round the fragments evenly");
+    // The chunks are stored in the first half of the rows.  LDS reads of the second half, which follow the last
+    // store, need not have returned when the step ends: what they read is overwritten two steps after the step that
+    // multiplies it.  (fp32 reads may be merged, so that their number is not known.)
+    constexpr int kHalf = FM / 2;
+    constexpr int kReads = AT == GASLOC_F32 ? 0 : kHalf * (OpA::kColumns ? 1 : 2) + FN / 2 * (OpB::kColumns ? 1 : 2);
 #pragma unroll
     for (int p = 0; p < 4; ++p) fa[p] = OpA::fragment(get_a, 0, p);
 #pragma unroll
@@ -313,7 +332,7 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
           for (int q = p * FN / FM; q < (p + 1) * FN / FM; ++q)
             fb[h ^ 1][q] = OpB::fragment(get_b, next * OpB::kLds, q);
 #pragma unroll
-          for (int j = p * (CA + CB) / FM; j < (p + 1) * (CA + CB) / FM; ++j) {
+          for (int j = p * (CA + CB) / kHalf; j < (p + 1) * (CA + CB) / kHalf && j < CA + CB; ++j) {
             if (j < CA) {
               oa.store(put_a + free * OpA::kLds, j, wa);
               oa.load(la, j, wa);
@@ -324,9 +343,11 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        __syncthreads();
+        step_barrier<kReads>();
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    __syncthreads();
   }
 
   // Lane l holds row l % 16 and columns 4 (l / 16) .. + 3 of each 16 x 16 block.  Sixteen rows at a time go
