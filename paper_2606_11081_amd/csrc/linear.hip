@@ -22,10 +22,16 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBuffers = 4;
-constexpr uint32_t kNowhere = 0xfffffff0u;  // an offset no buffer holds: the load gives zeros
+constexpr uint32_t kNowhere = 0x80000000u;  // no window holds this offset or one behind it: the load gives zeros
 
-// A range of memory that loads are checked against; what lies outside reads as zero.
+// A range of memory of at most 2^31 bytes that loads are checked against; what lies outside reads as zero.
+// (Both are the same in every lane; left to find that out, the compiler loops over the lanes' values.)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* p, uint32_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+  p = reinterpret_cast<const void*>(static_cast<uint64_t>(hi) << 32 | lo);
+  bytes = __builtin_amdgcn_readfirstlane(bytes);
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(bytes), 0x00027000);
 }
 
@@ -46,8 +52,12 @@ __device__ __forceinline__ __attribute__((address_space(3))) T* lds_pointer(uint
 // KC: rows run along k in memory.  ST: type in memory, CT: type of the product.
 // VEC: 16-byte chunks lie on 16-byte boundaries and are inside or outside as a whole.
 //
-// In LDS a KC step is [row][64 bytes], its four chunks permuted by the row's
-// place among sixteen; other bf16 steps are [k][row], blocks of 32 bytes
+// Rows are loaded by whole 128-byte lines, which along k may be two steps at
+// once (64 bytes at a time take twice the requests to L2, which were what
+// bounded the loop).
+//
+// In LDS a KC step is [row][64 bytes], its four blocks of 16 permuted by the
+// row's place among sixteen; other bf16 steps are [k][row], blocks of 32 bytes
 // permuted by k; fp32 ones have their lines 16 bytes apart.  So neither the
 // writes nor the lanes that a fragment read serves at a time meet in a bank
 // (plain padding of 16 bytes per KC row cost as many cycles in conflicts again).
@@ -56,22 +66,23 @@ struct Operand {
   static constexpr bool kColumns = KC;
   static constexpr int kSize = CT == GASLOC_BF16 ? 2 : 4;  // bytes of an element in LDS
   static constexpr int kSrc = ST == GASLOC_BF16 ? 2 : 4;   // and in memory
-  static constexpr int E = 16 / kSize;                     // elements of a chunk in LDS
-  static constexpr int KT = 4 * E;                         // k per step
-  static constexpr int kChunks = ROWS * 4 / THREADS;       // chunks per thread
-  static constexpr int kWords = E * kSrc / 4;              // words of a chunk in memory
-  static constexpr int kAcross = ROWS / E;                 // chunks of a [k][row] line
+  static constexpr int KT = 64 / kSize;                    // k per step
+  static constexpr int kSpan = KC && ST == CT ? 2 : 1;     // steps per load
+  static constexpr int E = 16 / kSrc;                      // elements of a chunk: 16 bytes in memory
+  static constexpr int kAcross = KC ? 8 : ROWS / E;        // chunks of a line in memory
+  static constexpr int kLines = THREADS / kAcross;         // lines between a thread's chunks
+  static constexpr int kChunks = (KC ? ROWS : KT) / kLines;
   static constexpr int kStride = KC ? 64 : ROWS * kSize + (CT == GASLOC_BF16 ? 0 : 16);
   static constexpr int kLds = KC ? ROWS * kStride : KT * kStride;
 
-  const char* at;  // row 0 of the step to be loaded next
+  const char* at;  // row 0 of the load to come
   int left;        // k from there on
-  int64_t ahead;   // bytes to the next step
+  int64_t ahead;   // bytes to the load after it
   uint32_t line;   // bytes between lines in memory
   int rows;        // rows inside (of ROWS)
-  uint32_t full;   // bytes of a whole step (not KC) or of the rows from `at` on (KC)
-  uint32_t off[kChunks];
-  typedef uint32_t Words[kChunks][kWords];  // a step on its way to LDS
+  uint32_t full;   // bytes of a whole load (not KC) or of the rows from `at` on (KC)
+  uint32_t off;    // of chunk 0 of this thread
+  typedef uint32_t Words[kChunks][4];  // a load on its way to LDS
 
   // p: element (first, 0) of the operand; `rows_left` rows from there on exist
   __device__ __forceinline__ void start(const void* p, int64_t ld, int rows_left, int k) {
@@ -79,75 +90,64 @@ struct Operand {
     line = static_cast<uint32_t>(ld * kSrc);
     rows = rows_left < ROWS ? rows_left : ROWS;
     left = k;
-    ahead = KC ? KT * kSrc : KT * static_cast<int64_t>(line);
+    ahead = KC ? kSpan * KT * kSrc : KT * static_cast<int64_t>(line);
     full = KC ? static_cast<uint32_t>(rows - 1) * line + static_cast<uint32_t>(k) * kSrc
               : static_cast<uint32_t>(KT - 1) * line + static_cast<uint32_t>(rows) * kSrc;
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      off[j] = static_cast<uint32_t>(row_of(j)) * line + static_cast<uint32_t>(col_of() * kSrc);
-      if (!KC && VEC && col_of() >= rows) off[j] = kNowhere;
-    }
+    off = static_cast<uint32_t>(line_of(0)) * line + static_cast<uint32_t>(col_of() * kSrc);
+    if (!KC && VEC && col_of() >= rows) off = kNowhere;
   }
   // The chunk j of this thread: its line in memory (a row of m or n, or of k) and its first column.
-  __device__ __forceinline__ int row_of(int j) const {
-    const int t = threadIdx.x;
-    return KC ? t / 4 + THREADS / 4 * j : t / kAcross + THREADS / kAcross * j;
-  }
-  __device__ __forceinline__ int col_of() const {
-    const int t = threadIdx.x;
-    return E * (KC ? t % 4 : t % kAcross);
-  }
+  __device__ __forceinline__ int line_of(int j) const { return static_cast<int>(threadIdx.x) / kAcross + kLines * j; }
+  __device__ __forceinline__ int col_of() const { return static_cast<int>(threadIdx.x) % kAcross * E; }
 
-  struct Step {
+  struct Load {
     __amdgpu_buffer_rsrc_t w;
     int lines, limit;  // lines and columns inside
   };
-  // The memory of the next step; `at` moves on.  Behind the last step nothing is inside.
-  __device__ __forceinline__ Step next() {
-    const int inside = left < 0 ? 0 : left < KT ? left : KT;
+  // The memory of the next load; `at` moves on.  Behind the last step nothing is inside.
+  __device__ __forceinline__ Load next() {
+    const int inside = max(0, min(left, KT));
     const uint32_t bytes = KC ? full : full - static_cast<uint32_t>(KT - inside) * line;
-    const Step s{window(at, left > 0 ? bytes : 0), KC ? rows : inside, KC ? left : rows};
-    if (KC) full -= KT * kSrc;
+    const Load l{window(at, left > 0 ? bytes : 0), KC ? rows : inside, KC ? left : rows};
+    if (KC) full -= kSpan * KT * kSrc;
     at += ahead;
-    left -= KT;
-    return s;
+    left -= kSpan * KT;
+    return l;
   }
 
-  // Chunk j of a step: into registers, then into LDS.
-  __device__ __forceinline__ void load(const Step& s, int j, Words& words) const {
+  // Chunk j of a load: into registers, then into LDS.
+  __device__ __forceinline__ void load(const Load& l, int j, Words& words) const {
     const int col = col_of();
+    const uint32_t down = static_cast<uint32_t>(j * kLines) * line;
     if constexpr (VEC) {
-      const uint32_t o = KC && col >= s.limit ? kNowhere : off[j];
+      const uint32_t o = (KC && col >= l.limit ? kNowhere : off) + down;
+      const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.w, o, 0, 0));
 #pragma unroll
-      for (int q = 0; q < kWords; q += 4) {
-        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(s.w, o + 4 * q, 0, 0));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) words[j][q + e] = v[e];
-      }
+      for (int e = 0; e < 4; ++e) words[j][e] = v[e];
     } else {
-      const bool inside = row_of(j) < s.lines;
+      const bool inside = line_of(j) < l.lines;
       uint32_t e[E];
 #pragma unroll
       for (int q = 0; q < E; ++q) {
-        const uint32_t o = inside && col + q < s.limit ? off[j] + q * kSrc : kNowhere;
+        const uint32_t o = inside && col + q < l.limit ? off + down + q * kSrc : kNowhere;
         if constexpr (ST == GASLOC_BF16)
-          e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(s.w, o, 0, 0));
+          e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(l.w, o, 0, 0));
         else
-          e[q] = __builtin_amdgcn_raw_buffer_load_b32(s.w, o, 0, 0);
+          e[q] = __builtin_amdgcn_raw_buffer_load_b32(l.w, o, 0, 0);
       }
 #pragma unroll
-      for (int q = 0; q < kWords; ++q) words[j][q] = ST == GASLOC_BF16 ? e[2 * q] | e[2 * q + 1] << 16 : e[q];
+      for (int q = 0; q < 4; ++q) words[j][q] = ST == GASLOC_BF16 ? e[2 * q % E] | e[(2 * q + 1) % E] << 16 : e[q % E];
     }
   }
-  // LDS addresses: where chunk 0 of this thread goes (chunk j lies kChunkStep further on), and the lane's part of the
-  // fragment that begins at row `row` of the tile.
-  static constexpr int kChunkStep = (KC ? THREADS / 4 : THREADS / kAcross) * kStride;
+  // Where chunk 0 of this thread goes, and the lane's part of the fragment that begins at row `row` of the tile.
   __device__ __forceinline__ uint32_t store_at(uint32_t lds) const {
-    const int row = row_of(0), chunk = col_of() / E;
-    const int to = KC                     ? (chunk ^ (0 - row / 4 & 3)) * 16
-                   : CT == GASLOC_BF16 ? ((chunk / 2 ^ across(row)) * 2 + chunk % 2) * 16
-                                       : chunk * 16;
-    return lds + row * kStride + to;
+    const int l = line_of(0), byte = col_of() * kSize;
+    if constexpr (KC)
+      return lds + byte / 64 * kLds + l * kStride + (byte % 64 / 16 ^ (0 - l / 4 & 3)) * 16 + byte % 16;
+    else if constexpr (CT == GASLOC_BF16)
+      return lds + l * kStride + (byte / 32 ^ across(l)) * 32 + byte % 32;
+    else
+      return lds + l * kStride + byte;
   }
   __device__ __forceinline__ static uint32_t read_at(uint32_t lds, int row) {
     const int l = lane_id(), i = l % 16, g = l / 16;
@@ -162,15 +162,17 @@ struct Operand {
   __device__ __forceinline__ static int across(int k) { return k % 4 + k / 8 % 2 * 4; }
 
   __device__ __forceinline__ void store(uint32_t to, int j, const Words& words) const {
-    static_assert(KC || CT != GASLOC_BF16 || THREADS / kAcross % 16 == 0 || kChunks == 1,
-                  "the chunks of a thread are permuted alike");
-    u32x4 v;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      v[q] = ST == CT ? words[j][q < kWords ? q : 0]
-                      : f32x2_to_bf16x2(__uint_as_float(words[j][(2 * q) % kWords]),
-                                        __uint_as_float(words[j][(2 * q + 1) % kWords]));
-    *lds_pointer<u32x4>(to + j * kChunkStep) = v;
+    static_assert(!KC || kLines % 16 == 0, "a thread's rows are permuted alike");
+    static_assert(KC || CT != GASLOC_BF16 || kLines % 8 == 0, "or by turns");
+    // line k + 8 has its blocks exchanged by fours
+    if (!KC && CT == GASLOC_BF16 && kLines * j / 8 % 2 == 1) to ^= 128;
+    to += j * kLines * kStride;
+    if constexpr (ST == CT) {
+      *lds_pointer<u32x4>(to) = u32x4{words[j][0], words[j][1], words[j][2], words[j][3]};
+    } else {
+      *lds_pointer<u32x2>(to) = u32x2{f32x2_to_bf16x2(__uint_as_float(words[j][0]), __uint_as_float(words[j][1])),
+                                      f32x2_to_bf16x2(__uint_as_float(words[j][2]), __uint_as_float(words[j][3]))};
+    }
   }
   // The fragment of sixteen rows, the p-th from the row `from` was made for: lane l has row l % 16, elements
   // E (l / 16) .. of the step's k.  `buffer`: how far the step's buffer lies behind the first.
@@ -270,10 +272,10 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   }
 
   if (depth > 0) {
-    // In step k its fragments are multiplied, those of step k + 1 are read from the next buffer, step k + 2 is
-    // stored into the one after it, and step k + 3 is loaded: all of it in between the rows of products, so that
-    // the matrix cores do not wait for any of it.  Behind the last step loads give zeros: there is no branch in the
-    // loop.
+    // In step k its fragments are multiplied, those of step k + 1 are read from the next buffer, step k + 2 (and k + 3,
+    // of an operand that is loaded two steps at a time, in even steps) is stored into the buffers after it, and what
+    // follows is loaded: all of it in between the rows of products, so that the matrix cores do not wait for any of
+    // it.  Behind the last step loads give zeros: there is no branch in the loop.
     constexpr int CA = OpA::kChunks, CB = OpB::kChunks;
     const uint32_t put_a = oa.store_at(lds_a), put_b = ob.store_at(lds_b);
     const uint32_t get_a = OpA::read_at(lds_a, wm), get_b = OpB::read_at(lds_b, wn);
@@ -282,25 +284,34 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
     {
       typename OpA::Words wa0, wa1;
       typename OpB::Words wb0, wb1;
-      const auto load_step = [&](typename OpA::Words& to_a, typename OpB::Words& to_b) {
-        const auto la = oa.next();
-        const auto lb = ob.next();
+      const auto load_a = [&](typename OpA::Words& to) {
+        const auto l = oa.next();
 #pragma unroll
-        for (int j = 0; j < CA; ++j) oa.load(la, j, to_a);
-#pragma unroll
-        for (int j = 0; j < CB; ++j) ob.load(lb, j, to_b);
+        for (int j = 0; j < CA; ++j) oa.load(l, j, to);
       };
-      load_step(wa0, wb0);
-      load_step(wa1, wb1);
-      load_step(wa, wb);
+      const auto load_b = [&](typename OpB::Words& to) {
+        const auto l = ob.next();
+#pragma unroll
+        for (int j = 0; j < CB; ++j) ob.load(l, j, to);
+      };
+      load_a(wa0);
+      load_b(wb0);
+      if (OpA::kSpan == 1) load_a(wa1);
+      if (OpB::kSpan == 1) load_b(wb1);
+      load_a(wa);
+      load_b(wb);
 #pragma unroll
       for (int j = 0; j < CA; ++j) oa.store(put_a, j, wa0);
 #pragma unroll
       for (int j = 0; j < CB; ++j) ob.store(put_b, j, wb0);
+      if (OpA::kSpan == 1) {
 #pragma unroll
-      for (int j = 0; j < CA; ++j) oa.store(put_a + OpA::kLds, j, wa1);
+        for (int j = 0; j < CA; ++j) oa.store(put_a + OpA::kLds, j, wa1);
+      }
+      if (OpB::kSpan == 1) {
 #pragma unroll
-      for (int j = 0; j < CB; ++j) ob.store(put_b + OpB::kLds, j, wb1);
+        for (int j = 0; j < CB; ++j) ob.store(put_b + OpB::kLds, j, wb1);
+      }
     }
     __syncthreads();
     u32x4 fa[4], fb[2][FN];  // A's fragments are read four rows ahead
@@ -320,8 +331,11 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
       for (int cur = 0; cur < kBuffers; ++cur) {
         constexpr int kMask = kBuffers - 1;
         const int next = cur + 1 & kMask, free = cur + 2 & kMask, h = cur & 1;
-        const auto la = oa.next();
-        const auto lb = ob.next();
+        const bool do_a = OpA::kSpan == 1 || h == 0, do_b = OpB::kSpan == 1 || h == 0;
+        typename OpA::Load la;
+        typename OpB::Load lb;
+        if (do_a) la = oa.next();
+        if (do_b) lb = ob.next();
 #pragma unroll
         for (int p = 0; p < FM; ++p) {
 #pragma unroll
@@ -332,14 +346,14 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
           for (int q = p * FN / FM; q < (p + 1) * FN / FM; ++q)
             fb[h ^ 1][q] = OpB::fragment(get_b, next * OpB::kLds, q);
 #pragma unroll
-          for (int j = p * (CA + CB) / kHalf; j < (p + 1) * (CA + CB) / kHalf && j < CA + CB; ++j) {
-            if (j < CA) {
-              oa.store(put_a + free * OpA::kLds, j, wa);
-              oa.load(la, j, wa);
-            } else {
-              ob.store(put_b + free * OpB::kLds, j - CA, wb);
-              ob.load(lb, j - CA, wb);
-            }
+          for (int j = p * CA / kHalf; j < (p + 1) * CA / kHalf && j < CA && do_a; ++j) {
+            oa.store(put_a + free * OpA::kLds, j, wa);
+            oa.load(la, j, wa);
+          }
+#pragma unroll
+          for (int j = p * CB / kHalf; j < (p + 1) * CB / kHalf && j < CB && do_b; ++j) {
+            ob.store(put_b + free * OpB::kLds, j, wb);
+            ob.load(lb, j, wb);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
