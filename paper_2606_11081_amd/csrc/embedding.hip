@@ -17,8 +17,9 @@ namespace {
 // A wave takes kLookupRows consecutive rows.
 constexpr int kLookupRows = 4;
 
-template <int PT, int AT, int V>
+template <int PT, int AT>
 __global__ __launch_bounds__(256) void k_embedding(EmbeddingArgs a) {
+  constexpr int V = AT == GASLOC_BF16 ? 8 : 4;
   const int wave = blockIdx.x * (256 / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id();
   const int rows = a.rows.begin[a.n];
@@ -32,10 +33,10 @@ __global__ __launch_bounds__(256) void k_embedding(EmbeddingArgs a) {
     const int64_t at = a.begin + static_cast<int64_t>(real ? k : 0) * a.width;
     for (int c = lane * V; c < a.width; c += kWave * V) {
       float w[V];
-      load_cached<PT, V>(row, at + c, w);
+      load_row<PT, V, false>(row, at + c, a.width - c, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) w[e] = real ? a.scale * w[e] : 0.0f;
-      store_out<AT, V>(a.out, static_cast<int64_t>(t) * a.out_ld + c, w);
+      store_row<AT, V>(a.out, static_cast<int64_t>(t) * a.out_ld + c, a.width - c, w);
     }
   }
 }
@@ -165,6 +166,20 @@ __device__ __forceinline__ int count_below(const uint32_t* keys, int64_t lo, int
   return static_cast<int>(lo - start);
 }
 
+// The first entry of keys[lo, hi) that is not below `key` (hi if there is none), found by the whole wave: each step
+// asks 64 places at once.
+__device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t lo, int64_t hi, uint32_t key) {
+  while (lo < hi) {
+    const int64_t step = (hi - lo + kWave - 1) / kWave;
+    const int64_t at = lo + (lane_id() + 1) * step - 1;
+    const int below = __popcll(__ballot(at < hi && keys[at < hi ? at : lo] < key));
+    const int64_t next = lo + (below + 1) * step - 1;  // not below, or behind the end
+    lo += below * step;
+    hi = next < hi ? next : hi;
+  }
+  return lo;
+}
+
 // An entry's place in the merged run: its place in its own run, and how many
 // entries of each other run come first (of an earlier run also the equal ones).
 __global__ __launch_bounds__(256) void k_token_merge(MergeArgs a) {
@@ -186,7 +201,7 @@ __global__ __launch_bounds__(256) void k_token_merge(MergeArgs a) {
 }
 
 // (+)= scale * sum, for V columns of a table row
-template <int V>
+constexpr int V = 4;
 __device__ __forceinline__ void put_grad(const EmbeddingGradArgs& a, int i, uint32_t key, int c, const float (&sum)[V]) {
   float* g = a.grads + static_cast<int64_t>(i) * a.grad_ld + a.begin + static_cast<int64_t>(key) * a.width + c;
   float o[V];
@@ -194,34 +209,35 @@ __device__ __forceinline__ void put_grad(const EmbeddingGradArgs& a, int i, uint
   for (int e = 0; e < V; ++e) o[e] = a.scale * sum[e];
   if (a.accumulate) {
     float old[V];
-    load_once<GASLOC_F32, V>(g, 0, old);
+    load_row<GASLOC_F32, V, true>(g, 0, a.width - c, old);
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = old[e] + o[e];
   }
-  store_out<GASLOC_F32, V>(g, 0, o);
+  store_row<GASLOC_F32, V>(g, 0, a.width - c, o);
 }
 
-template <int AT, int V>
-__global__ void k_embedding_sums(EmbeddingGradArgs a) {
+template <int AT>
+__global__ __launch_bounds__(256) void k_embedding_sums(EmbeddingGradArgs a) {
   __shared__ uint32_t s_key[kMaxChunk + 2];  // with the entries before and behind the chunk
   __shared__ int32_t s_pos[kMaxChunk];
   const int tid = threadIdx.x, threads = blockDim.x;
   const int b = blockIdx.x, chunks = a.chunks.begin[a.n];
   if (b >= chunks) {  // zero the rows of [k0, k1) that have no token
-    const int per = (a.vocab + kFillRows - 1) / kFillRows;
+    const int per = (a.vocab + a.fill_rows - 1) / a.fill_rows;
     const int i = (b - chunks) / per;
-    const int k0 = (b - chunks) % per * kFillRows, k1 = min(k0 + kFillRows, a.vocab);
-    const int64_t lo = a.rows.begin[i], hi = a.rows.begin[i + 1];
-    for (int k = k0 + tid; k < k1; k += threads) {
-      const int64_t at = lo + count_below(a.keys, lo, hi, static_cast<uint32_t>(k), false);
-      s_key[k - k0] = at < hi && a.keys[at] == static_cast<uint32_t>(k);
-    }
+    const int k0 = (b - chunks) % per * a.fill_rows, k1 = min(k0 + a.fill_rows, a.vocab);
+    const int64_t end = a.rows.begin[i + 1];
+    const int64_t lo = lower_bound(a.keys, a.rows.begin[i], end, static_cast<uint32_t>(k0));
+    const int64_t hi = lower_bound(a.keys, lo, end, static_cast<uint32_t>(k1));
+    for (int k = tid; k < k1 - k0; k += threads) s_key[k] = 0;
+    __syncthreads();
+    for (int64_t e = lo + tid; e < hi; e += threads) s_key[a.keys[e] - static_cast<uint32_t>(k0)] = 1;
     __syncthreads();
     const float zero[V] = {};
     for (int k = k0; k < k1; ++k) {
       if (s_key[k - k0]) continue;
       float* g = a.grads + static_cast<int64_t>(i) * a.grad_ld + a.begin + static_cast<int64_t>(k) * a.width;
-      for (int c = tid * V; c < a.width; c += threads * V) store_out<GASLOC_F32, V>(g, c, zero);
+      for (int c = tid * V; c < a.width; c += threads * V) store_row<GASLOC_F32, V>(g, c, a.width - c, zero);
     }
     return;
   }
@@ -245,7 +261,7 @@ __global__ void k_embedding_sums(EmbeddingGradArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int at = min(e0 + e, count - 1);
-        load_once<AT, V>(a.dout, static_cast<int64_t>(s_pos[at]) * a.dout_ld + c, v[e]);
+        load_row<AT, V, true>(a.dout, static_cast<int64_t>(s_pos[at]) * a.dout_ld + c, a.width - c, v[e]);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -259,9 +275,10 @@ __global__ void k_embedding_sums(EmbeddingGradArgs a) {
             if (key < static_cast<uint32_t>(a.vocab)) {
               const bool tail = last && behind;
               if (!head && !tail)
-                put_grad<V>(a, i, key, c, sum);
+                put_grad(a, i, key, c, sum);
               else
-                store_out<GASLOC_F32, V>(a.partial, (2 * static_cast<int64_t>(b) + (head ? 0 : 1)) * a.width + c, sum);
+                store_row<GASLOC_F32, V>(a.partial, (2 * static_cast<int64_t>(b) + (head ? 0 : 1)) * a.width + c,
+                                         a.width - c, sum);
             }
 #pragma unroll
             for (int q = 0; q < V; ++q) sum[q] = 0.0f;
@@ -274,28 +291,33 @@ __global__ void k_embedding_sums(EmbeddingGradArgs a) {
 }
 
 // Finishes the row that begins in chunk b and goes on behind it: its part
-// here, then its parts in the chunks that follow, in order.
-template <int V>
-__global__ void k_embedding_join(EmbeddingGradArgs a) {
+// here, then its parts in the chunks that follow, in order.  It goes on into
+// chunk q as long as q begins with it: 64 chunks are asked at a time.
+__global__ __launch_bounds__(256) void k_embedding_join(EmbeddingGradArgs a) {
   const int b = blockIdx.x;
   const int i = find_worker(a.chunks, a.n, b);
   const int begin = a.rows.begin[i], end = a.rows.begin[i + 1];
   const int first = begin + (b - a.chunks.begin[i]) * a.chunk;
   const int next = first + a.chunk;
   if (next >= end) return;
-  const uint32_t key = a.keys[next - 1];
+  const uint32_t key = a.keys[next - 1], head = a.keys[first], before = a.keys[first > begin ? first - 1 : first];
   if (key >= static_cast<uint32_t>(a.vocab) || a.keys[next] != key) return;
-  if (a.keys[first] == key && first > begin && a.keys[first - 1] == key) return;  // began earlier
-  const int stop = next + count_below(a.keys, next, end, key, true);
-  const int last = b + (stop - 1 - first) / a.chunk;
+  if (head == key && first > begin && before == key) return;  // began earlier
+  int last = b;
+  for (int more = kWave; more == kWave; last += more) {
+    const int64_t at = first + static_cast<int64_t>(last - b + 1 + lane_id()) * a.chunk;
+    const uint64_t goes_on = __ballot(at < end && a.keys[at < end ? at : first] == key);
+    more = goes_on == ~0ull ? kWave : __builtin_ctzll(~goes_on);
+  }
   for (int c = threadIdx.x * V; c < a.width; c += blockDim.x * V) {
     float sum[V];
-    load_once<GASLOC_F32, V>(a.partial, (2 * static_cast<int64_t>(b) + 1) * a.width + c, sum);
+    load_row<GASLOC_F32, V, true>(a.partial, (2 * static_cast<int64_t>(b) + 1) * a.width + c, a.width - c, sum);
     for (int q0 = b + 1; q0 <= last; q0 += 8) {
       float v[8][V];
 #pragma unroll
       for (int q = 0; q < 8; ++q)
-        load_once<GASLOC_F32, V>(a.partial, 2 * static_cast<int64_t>(min(q0 + q, last)) * a.width + c, v[q]);
+        load_row<GASLOC_F32, V, true>(a.partial, 2 * static_cast<int64_t>(min(q0 + q, last)) * a.width + c,
+                                      a.width - c, v[q]);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         if (q0 + q <= last) {
@@ -304,31 +326,25 @@ __global__ void k_embedding_join(EmbeddingGradArgs a) {
         }
       }
     }
-    put_grad<V>(a, i, key, c, sum);
+    put_grad(a, i, key, c, sum);
   }
 }
 
-// Threads for a row of `width` columns, V at a time.
-int row_threads(int width, int v) {
-  const int need = (width + v - 1) / v;
+// Threads for a row of `width` columns.
+int row_threads(int width) {
+  const int need = (width + V - 1) / V;
   return need > 128 ? 256 : need > 64 ? 128 : 64;
-}
-
-template <int PT, int AT>
-hipError_t lookup(const EmbeddingArgs& a, bool vec, hipStream_t stream) {
-  const int rows = a.rows.begin[a.n];
-  constexpr int per = kLookupRows * 256 / kWave;
-  const dim3 grid((rows + per - 1) / per);
-  constexpr int V = AT == GASLOC_BF16 ? 8 : 4;
-  return launch_kernel(vec ? k_embedding<PT, AT, V> : k_embedding<PT, AT, 1>, grid, 256, 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_embedding(const EmbeddingArgs& a, int params, int act, bool vec, hipStream_t stream) {
-  if (params == GASLOC_BF16) return lookup<GASLOC_BF16, GASLOC_BF16>(a, vec, stream);
-  if (act == GASLOC_BF16) return lookup<GASLOC_F32, GASLOC_BF16>(a, vec, stream);
-  return lookup<GASLOC_F32, GASLOC_F32>(a, vec, stream);
+hipError_t launch_embedding(const EmbeddingArgs& a, int params, int act, hipStream_t stream) {
+  const int rows = a.rows.begin[a.n];
+  constexpr int per = kLookupRows * 256 / kWave;
+  return launch_kernel(params == GASLOC_BF16 ? k_embedding<GASLOC_BF16, GASLOC_BF16>
+                       : act == GASLOC_BF16  ? k_embedding<GASLOC_F32, GASLOC_BF16>
+                                             : k_embedding<GASLOC_F32, GASLOC_F32>,
+                       dim3((rows + per - 1) / per), 256, 0, stream, a);
 }
 
 hipError_t launch_token_sort(const SortArgs& a, hipStream_t stream) {
@@ -339,19 +355,14 @@ hipError_t launch_token_merge(const MergeArgs& a, hipStream_t stream) {
   return launch_kernel(k_token_merge, dim3(a.blocks.begin[a.n]), 256, 0, stream, a);
 }
 
-hipError_t launch_embedding_sums(const EmbeddingGradArgs& a, int act, bool vec, hipStream_t stream) {
-  const int fill = a.accumulate ? 0 : a.n * ((a.vocab + kFillRows - 1) / kFillRows);
-  const dim3 grid(a.chunks.begin[a.n] + fill);
-  if (act == GASLOC_BF16)
-    return launch_kernel(vec ? k_embedding_sums<GASLOC_BF16, 8> : k_embedding_sums<GASLOC_BF16, 1>, grid,
-                         row_threads(a.width, vec ? 8 : 1), 0, stream, a);
-  return launch_kernel(vec ? k_embedding_sums<GASLOC_F32, 4> : k_embedding_sums<GASLOC_F32, 1>, grid,
-                       row_threads(a.width, vec ? 4 : 1), 0, stream, a);
+hipError_t launch_embedding_sums(const EmbeddingGradArgs& a, int act, hipStream_t stream) {
+  const int fill = a.accumulate ? 0 : a.n * ((a.vocab + a.fill_rows - 1) / a.fill_rows);
+  return launch_kernel(act == GASLOC_BF16 ? k_embedding_sums<GASLOC_BF16> : k_embedding_sums<GASLOC_F32>,
+                       dim3(a.chunks.begin[a.n] + fill), row_threads(a.width), 0, stream, a);
 }
 
-hipError_t launch_embedding_join(const EmbeddingGradArgs& a, bool vec, hipStream_t stream) {
-  return launch_kernel(vec ? k_embedding_join<4> : k_embedding_join<1>, dim3(a.chunks.begin[a.n]),
-                       row_threads(a.width, vec ? 4 : 1), 0, stream, a);
+hipError_t launch_embedding_join(const EmbeddingGradArgs& a, hipStream_t stream) {
+  return launch_kernel(k_embedding_join, dim3(a.chunks.begin[a.n]), row_threads(a.width), 0, stream, a);
 }
 
 }  // namespace gasloc

@@ -39,8 +39,8 @@ __device__ __forceinline__ void row_sums(float (&v)[K], int slot) {
   }
 }
 
-// E columns per thread, V consecutive ones at a time.
-template <int PT, int AT, int V, int E, int WAVES>
+// E columns per thread, V consecutive ones at a time; WHOLE: rows are whole vectors.
+template <int PT, int AT, int V, int E, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(NormArgs a) {
   constexpr int N = E / V, kStep = WAVES * kWave * V;
   constexpr int kRowsAtOnce = WAVES == 1 ? 4 : 1;
@@ -50,14 +50,15 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c0 = (WAVES == 1 ? lane_id() : static_cast<int>(threadIdx.x)) * V;
   const void* row = live_row<PT>(a.w, i);
+  const auto left = [&](int j) { return WHOLE ? V : a.width - (c0 + j * kStep); };
   const float inv = 1.0f / static_cast<float>(a.width);
   float gain[E], bias[E];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     float g[V] = {}, b[V] = {};
     if (c0 + j * kStep < a.width) {
-      load_cached<PT, V>(row, a.gain + c0 + j * kStep, g);
-      if (a.bias >= 0) load_cached<PT, V>(row, a.bias + c0 + j * kStep, b);
+      load_row<PT, V, false>(row, a.gain + c0 + j * kStep, left(j), g);
+      if (a.bias >= 0) load_row<PT, V, false>(row, a.bias + c0 + j * kStep, left(j), b);
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       float v[V] = {};
-      if (c0 + j * kStep < a.width) load_once<AT, V>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, v);
+      if (c0 + j * kStep < a.width) load_row<AT, V, true>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, left(j), v);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         x[j * V + e] = v[e];
@@ -83,12 +84,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(
     float sq[1] = {0.0f};
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const bool in = c0 + j * kStep < a.width;
+      const int inside = a.width - (c0 + j * kStep);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float d = x[j * V + e] - mean;
         x[j * V + e] = d;
-        if (in) sq[0] = fmaf(d, d, sq[0]);
+        if ((WHOLE ? 0 : e) < inside) sq[0] = fmaf(d, d, sq[0]);
       }
     }
     row_sums<WAVES, 1>(sq, 1);
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = fmaf(x[j * V + e] * rstd, gain[j * V + e], bias[j * V + e]);
       if (c0 + j * kStep < a.width)
-        store_out<AT, V>(a.out, static_cast<int64_t>(t) * a.out_ld + c0 + j * kStep, o);
+        store_row<AT, V>(a.out, static_cast<int64_t>(t) * a.out_ld + c0 + j * kStep, left(j), o);
     }
     if (a.stats && c0 == 0) {
       a.stats[2 * static_cast<int64_t>(t)] = mean;
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(
   }
 }
 
-template <int PT, int AT, int V, int E, int WAVES>
+template <int PT, int AT, int V, int E, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm_grad(NormGradArgs a) {
   constexpr int N = E / V, kStep = WAVES * kWave * V;
   constexpr int kRowsAtOnce = WAVES == 1 ? 4 : 1;
@@ -118,12 +119,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm_
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c0 = (WAVES == 1 ? lane_id() : static_cast<int>(threadIdx.x)) * V;
   const void* row = live_row<PT>(a.w, i);
+  const auto left = [&](int j) { return WHOLE ? V : a.width - (c0 + j * kStep); };
   const float inv = 1.0f / static_cast<float>(a.width);
   float gain[E], dgain[E] = {}, dbias[E] = {};
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     float g[V] = {};
-    if (c0 + j * kStep < a.width) load_cached<PT, V>(row, a.gain + c0 + j * kStep, g);
+    if (c0 + j * kStep < a.width) load_row<PT, V, false>(row, a.gain + c0 + j * kStep, left(j), g);
 #pragma unroll
     for (int e = 0; e < V; ++e) gain[j * V + e] = g[e];
   }
@@ -133,12 +135,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm_
     const float mean = a.stats[2 * static_cast<int64_t>(t)], rstd = a.stats[2 * static_cast<int64_t>(t) + 1];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      float v[V], d[V] = {};
+      float v[V], d[V] = {};  // columns behind the row count nothing in h, and xh is not used there
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = mean;  // columns behind the row: xh = 0
+      for (int e = 0; e < V; ++e) v[e] = mean;
       if (c0 + j * kStep < a.width) {
-        load_once<AT, V>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, v);
-        load_once<AT, V>(a.dout, static_cast<int64_t>(t) * a.dout_ld + c0 + j * kStep, d);
+        load_row<AT, V, true>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, left(j), v);
+        load_row<AT, V, true>(a.dout, static_cast<int64_t>(t) * a.dout_ld + c0 + j * kStep, left(j), d);
       }
 #pragma unroll
       for (int e = 0; e < V; ++e) {
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm_
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = rstd * ((h[j * V + e] - m1) - x[j * V + e] * m2);
       if (c0 + j * kStep < a.width)
-        store_out<AT, V>(a.dx, static_cast<int64_t>(t) * a.dx_ld + c0 + j * kStep, o);
+        store_row<AT, V>(a.dx, static_cast<int64_t>(t) * a.dx_ld + c0 + j * kStep, left(j), o);
     }
   }
   float* part = a.partial + 2 * static_cast<int64_t>(blockIdx.x) * a.width;
@@ -198,20 +200,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm_
       b[e] = dbias[j * V + e];
     }
     if (c0 + j * kStep < a.width) {
-      // the partials of an odd width are not aligned to whole vectors
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        part[c0 + j * kStep + e] = g[e];
-        part[a.width + c0 + j * kStep + e] = b[e];
-      }
+      store_row<GASLOC_F32, V>(part, c0 + j * kStep, left(j), g);
+      store_row<GASLOC_F32, V>(part, a.width + c0 + j * kStep, left(j), b);
     }
   }
 }
 
-// Adds the tiles' sums of one worker, in four stretches of tiles that are
+// Adds the tiles' sums of one worker, in sixteen stretches of tiles that are
 // then added in order: thread (g, l) takes stretch g of column 64 b + l.
-__global__ __launch_bounds__(256) void k_layer_norm_join(NormGradArgs a) {
-  __shared__ float s_sum[4][kWave];
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(kJoinWaves* kWave) void k_layer_norm_join(NormGradArgs a) {
+  __shared__ float s_sum[kJoinWaves][kWave];
   const int i = blockIdx.y;
   const int64_t begin = a.tiles.begin[i], count = a.tiles.begin[i + 1] - begin;
   const int lane = lane_id(), g = threadIdx.x / kWave;
@@ -222,12 +221,14 @@ __global__ __launch_bounds__(256) void k_layer_norm_join(NormGradArgs a) {
     const float* p = a.partial + 2 * begin * a.width + c;
     const int64_t stride = 2 * static_cast<int64_t>(a.width);
 #pragma unroll 8
-    for (int64_t q = count * g / 4; q < count * (g + 1) / 4; ++q) sum += p[q * stride];
+    for (int64_t q = count * g / kJoinWaves; q < count * (g + 1) / kJoinWaves; ++q) sum += p[q * stride];
   }
   s_sum[g][lane] = sum;
   __syncthreads();
   if (g != 0 || !in) return;
-  sum = ((s_sum[0][lane] + s_sum[1][lane]) + s_sum[2][lane]) + s_sum[3][lane];
+  sum = s_sum[0][lane];
+#pragma unroll
+  for (int k = 1; k < kJoinWaves; ++k) sum += s_sum[k][lane];
   const int64_t to = c < a.width ? a.gain + c : a.bias < 0 ? -1 : a.bias + (c - a.width);
   if (to < 0) return;
   float* out = a.grads + static_cast<int64_t>(i) * a.grad_ld + to;
@@ -248,29 +249,31 @@ NormShape norm_shape(int width) {
   return {32, 8};
 }
 
-template <int PT, int AT, int V>
+template <int PT, int AT, bool WHOLE>
 hipError_t forward(const NormArgs& a, hipStream_t stream) {
+  constexpr int V = AT == GASLOC_BF16 ? 8 : 4;
   const NormShape s = norm_shape(a.width);
   const dim3 grid(a.tiles.begin[a.n]);
   const int threads = s.waves == 1 ? 256 : s.waves * kWave;
-  return launch_kernel(s.waves == 8  ? k_layer_norm<PT, AT, V, 32, 8>
-                       : s.waves == 4 ? k_layer_norm<PT, AT, V, 32, 4>
-                       : s.e == 32    ? k_layer_norm<PT, AT, V, 32, 1>
-                       : s.e == 16    ? k_layer_norm<PT, AT, V, 16, 1>
-                                      : k_layer_norm<PT, AT, V, 8, 1>,
+  return launch_kernel(s.waves == 8   ? k_layer_norm<PT, AT, V, 32, 8, WHOLE>
+                       : s.waves == 4 ? k_layer_norm<PT, AT, V, 32, 4, WHOLE>
+                       : s.e == 32    ? k_layer_norm<PT, AT, V, 32, 1, WHOLE>
+                       : s.e == 16    ? k_layer_norm<PT, AT, V, 16, 1, WHOLE>
+                                      : k_layer_norm<PT, AT, V, 8, 1, WHOLE>,
                        grid, threads, 0, stream, a);
 }
 
-template <int PT, int AT, int V>
+template <int PT, int AT, bool WHOLE>
 hipError_t backward(const NormGradArgs& a, hipStream_t stream) {
+  constexpr int V = AT == GASLOC_BF16 ? 8 : 4;
   const NormShape s = norm_shape(a.width);
   const dim3 grid(a.tiles.begin[a.n]);
   const int threads = s.waves == 1 ? 256 : s.waves * kWave;
-  return launch_kernel(s.waves == 8  ? k_layer_norm_grad<PT, AT, V, 32, 8>
-                       : s.waves == 4 ? k_layer_norm_grad<PT, AT, V, 32, 4>
-                       : s.e == 32    ? k_layer_norm_grad<PT, AT, V, 32, 1>
-                       : s.e == 16    ? k_layer_norm_grad<PT, AT, V, 16, 1>
-                                      : k_layer_norm_grad<PT, AT, V, 8, 1>,
+  return launch_kernel(s.waves == 8   ? k_layer_norm_grad<PT, AT, V, 32, 8, WHOLE>
+                       : s.waves == 4 ? k_layer_norm_grad<PT, AT, V, 32, 4, WHOLE>
+                       : s.e == 32    ? k_layer_norm_grad<PT, AT, V, 32, 1, WHOLE>
+                       : s.e == 16    ? k_layer_norm_grad<PT, AT, V, 16, 1, WHOLE>
+                                      : k_layer_norm_grad<PT, AT, V, 8, 1, WHOLE>,
                        grid, threads, 0, stream, a);
 }
 
@@ -278,24 +281,25 @@ hipError_t backward(const NormGradArgs& a, hipStream_t stream) {
 
 int norm_waves(int width) { return norm_shape(width).waves; }
 
-hipError_t launch_layer_norm(const NormArgs& a, int params, int act, bool vec, hipStream_t stream) {
+hipError_t launch_layer_norm(const NormArgs& a, int params, int act, bool whole, hipStream_t stream) {
   if (params == GASLOC_BF16)
-    return vec ? forward<GASLOC_BF16, GASLOC_BF16, 8>(a, stream) : forward<GASLOC_BF16, GASLOC_BF16, 1>(a, stream);
+    return whole ? forward<GASLOC_BF16, GASLOC_BF16, true>(a, stream) : forward<GASLOC_BF16, GASLOC_BF16, false>(a, stream);
   if (act == GASLOC_BF16)
-    return vec ? forward<GASLOC_F32, GASLOC_BF16, 8>(a, stream) : forward<GASLOC_F32, GASLOC_BF16, 1>(a, stream);
-  return vec ? forward<GASLOC_F32, GASLOC_F32, 4>(a, stream) : forward<GASLOC_F32, GASLOC_F32, 1>(a, stream);
+    return whole ? forward<GASLOC_F32, GASLOC_BF16, true>(a, stream) : forward<GASLOC_F32, GASLOC_BF16, false>(a, stream);
+  return whole ? forward<GASLOC_F32, GASLOC_F32, true>(a, stream) : forward<GASLOC_F32, GASLOC_F32, false>(a, stream);
 }
 
-hipError_t launch_layer_norm_grad(const NormGradArgs& a, int params, int act, bool vec, hipStream_t stream) {
+hipError_t launch_layer_norm_grad(const NormGradArgs& a, int params, int act, bool whole, hipStream_t stream) {
   if (params == GASLOC_BF16)
-    return vec ? backward<GASLOC_BF16, GASLOC_BF16, 8>(a, stream) : backward<GASLOC_BF16, GASLOC_BF16, 1>(a, stream);
+    return whole ? backward<GASLOC_BF16, GASLOC_BF16, true>(a, stream) : backward<GASLOC_BF16, GASLOC_BF16, false>(a, stream);
   if (act == GASLOC_BF16)
-    return vec ? backward<GASLOC_F32, GASLOC_BF16, 8>(a, stream) : backward<GASLOC_F32, GASLOC_BF16, 1>(a, stream);
-  return vec ? backward<GASLOC_F32, GASLOC_F32, 4>(a, stream) : backward<GASLOC_F32, GASLOC_F32, 1>(a, stream);
+    return whole ? backward<GASLOC_F32, GASLOC_BF16, true>(a, stream) : backward<GASLOC_F32, GASLOC_BF16, false>(a, stream);
+  return whole ? backward<GASLOC_F32, GASLOC_F32, true>(a, stream) : backward<GASLOC_F32, GASLOC_F32, false>(a, stream);
 }
 
 hipError_t launch_layer_norm_join(const NormGradArgs& a, hipStream_t stream) {
-  return launch_kernel(k_layer_norm_join, dim3((2 * a.width + kWave - 1) / kWave, a.n), 256, 0, stream, a);
+  return launch_kernel(k_layer_norm_join, dim3((2 * a.width + kWave - 1) / kWave, a.n), kJoinWaves * kWave, 0,
+                       stream, a);
 }
 
 }  // namespace gasloc

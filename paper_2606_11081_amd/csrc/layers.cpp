@@ -113,10 +113,11 @@ Spans item_spans(int n, const int64_t* row_ptr, int64_t per) {
   return s;
 }
 
+bool whole_vectors(int64_t cols, int32_t dtype) { return cols % (dtype == GASLOC_BF16 ? 8 : 4) == 0; }
+
 // Rows of `cols` elements that begin on 16-byte boundaries and are whole 16-byte vectors.
 bool vector_rows(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
-  const int64_t v = dtype == GASLOC_BF16 ? 8 : 4;
-  return aligned16(p) && ld % v == 0 && cols % v == 0;
+  return aligned16(p) && whole_vectors(ld, dtype) && whole_vectors(cols, dtype);
 }
 
 // The same for a weight at column `begin` of the parameters and of the gradients.
@@ -128,8 +129,13 @@ size_t round256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 // embedding
 // ---------------------------------------------------------------------------
 
-// Sorted entries per workgroup of the sums: 32.
-int64_t sum_chunk(int64_t) { return 32; }
+// Sorted entries per workgroup of the sums: a power of two from 8 to 32, with which the rows make at least about two
+// workgroups per CU (256 of them) while there are enough.
+int64_t sum_chunk(int64_t rows) {
+  int64_t chunk = 32;
+  while (chunk > 8 && rows / chunk < 512) chunk /= 2;
+  return chunk;
+}
 
 struct EmbeddingSpace {
   size_t keys[2], pos[2], partial, bytes;
@@ -279,10 +285,8 @@ gasloc_status gasloc_embedding(gasloc_ctx* c, int64_t begin, int32_t vocab, int3
     a.out = out;
     a.out_ld = out_ld;
     a.rows = row_spans(c->n, row_ptr);
-    // a table row is as wide as a vector of the activations' type, which is no shorter in parameters
-    const bool vec = vector_rows(out, out_ld, width, dtype) && vector_columns(*c, begin);
     DeviceGuard guard(c->device);
-    HIP_TRY(c, gasloc::launch_embedding(a, c->hp.param_dtype, dtype, vec, c->stream));
+    HIP_TRY(c, gasloc::launch_embedding(a, c->hp.param_dtype, dtype, c->stream));
     return GASLOC_OK;
   });
 }
@@ -365,11 +369,11 @@ gasloc_status gasloc_embedding_grad(gasloc_ctx* c, int64_t begin, int32_t vocab,
     a.accumulate = accumulate;
     a.rows = row_spans(n, row_ptr);
     a.chunks = item_spans(n, row_ptr, a.chunk);
-    const bool grads_vec = begin % 4 == 0 && width % 4 == 0;
-    // eight columns at a time from BF16 rows, so the gradients' rows are whole vectors too
-    const bool vec = grads_vec && vector_rows(dout, dout_ld, width, dtype);
-    HIP_TRY(c, gasloc::launch_embedding_sums(a, dtype, vec, c->stream));
-    if (rows > a.chunk) HIP_TRY(c, gasloc::launch_embedding_join(a, grads_vec, c->stream));
+    // Rows without tokens are zeroed about 16 KB to a workgroup, in the order of the rows: what is written at any
+    // time is one stretch of memory (1 MB each, n = 16 tables of 32000 x 1024: 454 us; 256 KB: 436; 16 KB: 358 us).
+    a.fill_rows = static_cast<int32_t>(std::min<int64_t>(gasloc::kMaxChunk, std::max<int64_t>(1, 4096 / width)));
+    HIP_TRY(c, gasloc::launch_embedding_sums(a, dtype, c->stream));
+    if (rows > a.chunk) HIP_TRY(c, gasloc::launch_embedding_join(a, c->stream));
     return GASLOC_OK;
   });
 }
@@ -401,13 +405,11 @@ gasloc_status gasloc_layer_norm(gasloc_ctx* c, int64_t gain, int64_t bias, int32
     a.out = out;
     a.out_ld = out_ld;
     a.stats = stats;
-    const bool vec = vector_rows(x, x_ld, width, dtype) && vector_rows(out, out_ld, width, dtype) &&
-                     vector_columns(*c, gain) && (bias < 0 || vector_columns(*c, bias));
     a.tile_rows = static_cast<int32_t>(forward_tile_rows(*c, rows, gasloc::norm_waves(width)));
     a.rows = row_spans(c->n, row_ptr);
     a.tiles = item_spans(c->n, row_ptr, a.tile_rows);
     DeviceGuard guard(c->device);
-    HIP_TRY(c, gasloc::launch_layer_norm(a, c->hp.param_dtype, dtype, vec, c->stream));
+    HIP_TRY(c, gasloc::launch_layer_norm(a, c->hp.param_dtype, dtype, whole_vectors(width, dtype), c->stream));
     return GASLOC_OK;
   });
 }
@@ -465,13 +467,12 @@ gasloc_status gasloc_layer_norm_grad(gasloc_ctx* c, int64_t gain, int64_t bias, 
     a.partial = static_cast<float*>(workspace);
     a.grads = grads;
     a.grad_ld = grad_ld;
-    const bool vec = vector_rows(x, x_ld, width, dtype) && vector_rows(dout, dout_ld, width, dtype) &&
-                     vector_rows(dx, dx_ld, width, dtype) && vector_columns(*c, gain);
     a.tile_rows = static_cast<int32_t>(backward_tile_rows(*c, rows, gasloc::norm_waves(width)));
     a.rows = row_spans(c->n, row_ptr);
     a.tiles = item_spans(c->n, row_ptr, a.tile_rows);
     DeviceGuard guard(c->device);
-    if (rows > 0) HIP_TRY(c, gasloc::launch_layer_norm_grad(a, c->hp.param_dtype, dtype, vec, c->stream));
+    if (rows > 0)
+      HIP_TRY(c, gasloc::launch_layer_norm_grad(a, c->hp.param_dtype, dtype, whole_vectors(width, dtype), c->stream));
     HIP_TRY(c, gasloc::launch_layer_norm_join(a, c->stream));
     return GASLOC_OK;
   });

@@ -35,7 +35,7 @@ struct EmbeddingArgs {
   int64_t out_ld;
   Spans rows;
 };
-hipError_t launch_embedding(const EmbeddingArgs& a, int params, int act, bool vec, hipStream_t stream);
+hipError_t launch_embedding(const EmbeddingArgs& a, int params, int act, hipStream_t stream);
 
 // Gradient of the table.  Tokens are sorted per worker: first tiles of kSortTile
 // rows each in LDS, then kMergeWays sorted runs at a time into one.
@@ -68,7 +68,6 @@ hipError_t launch_token_merge(const MergeArgs& a, hipStream_t stream);
 // the sums of rows that go over an edge of it are left in partial[chunk][0]
 // (the row began before) or [1] (it began here) and added up by the join.
 // Workgroups from chunks.begin[n] on zero table rows without tokens.
-constexpr int kFillRows = 64;  // table rows per zeroing workgroup
 constexpr int kMaxChunk = 256;
 struct EmbeddingGradArgs {
   const uint32_t* keys;
@@ -81,10 +80,11 @@ struct EmbeddingGradArgs {
   float* partial;  // [chunks][2][width]
   float scale;
   int32_t vocab, width, n, chunk, accumulate;
+  int32_t fill_rows;  // table rows per zeroing workgroup, at most kMaxChunk
   Spans rows, chunks;
 };
-hipError_t launch_embedding_sums(const EmbeddingGradArgs& a, int act, bool vec, hipStream_t stream);
-hipError_t launch_embedding_join(const EmbeddingGradArgs& a, bool vec, hipStream_t stream);
+hipError_t launch_embedding_sums(const EmbeddingGradArgs& a, int act, hipStream_t stream);
+hipError_t launch_embedding_join(const EmbeddingGradArgs& a, hipStream_t stream);
 
 constexpr int kMaxNormWidth = 16384;
 struct NormArgs {
@@ -100,7 +100,8 @@ struct NormArgs {
   float* stats;
   Spans rows, tiles;
 };
-hipError_t launch_layer_norm(const NormArgs& a, int params, int act, bool vec, hipStream_t stream);
+// whole: widths are a multiple of 8 (bf16 rows) or 4 (fp32).
+hipError_t launch_layer_norm(const NormArgs& a, int params, int act, bool whole, hipStream_t stream);
 // Waves that share a row of this width.
 int norm_waves(int width);
 
@@ -122,7 +123,7 @@ struct NormGradArgs {
   int64_t grad_ld;
   Spans rows, tiles;
 };
-hipError_t launch_layer_norm_grad(const NormGradArgs& a, int params, int act, bool vec, hipStream_t stream);
+hipError_t launch_layer_norm_grad(const NormGradArgs& a, int params, int act, bool whole, hipStream_t stream);
 hipError_t launch_layer_norm_join(const NormGradArgs& a, hipStream_t stream);
 
 // Linear layers: for every worker C[m][n] = sum_k A(m, k) B(n, k), the rows of

@@ -27,68 +27,119 @@ __device__ __forceinline__ const void* live_row(const LiveRows& w, int i) {
   return static_cast<const char*>(base) + static_cast<int64_t>(i) * w.ld * (PT == GASLOC_BF16 ? 2 : 4);
 }
 
-// V consecutive elements through the caches (16-byte aligned where V elements are 16 bytes or more).
-template <int DT, int V>
-__device__ __forceinline__ void load_cached(const void* base, int64_t idx, float (&o)[V]) {
+// ---------------------------------------------------------------------------
+// V consecutive elements (4 or 8) of a row, at any alignment of the element:
+// the memory instructions of gfx950 take 16 bytes at any address.  `left`:
+// elements of the row from the first one on; those behind it are left out
+// (read as zero).  Whole rows of vectors pass left = V.
+// ---------------------------------------------------------------------------
+
+// Four or two words at an address of any alignment of two bytes; STREAM: data that is touched once.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_words4(const void* p) {
+  const u32x4_any* q = static_cast<const u32x4_any*>(p);
+  if constexpr (STREAM && GASLOC_NONTEMPORAL)
+    return __builtin_nontemporal_load(q);
+  else
+    return *q;
+}
+template <bool STREAM>
+__device__ __forceinline__ u32x2 load_words2(const void* p) {
+  const u32x2_any* q = static_cast<const u32x2_any*>(p);
+  if constexpr (STREAM && GASLOC_NONTEMPORAL)
+    return __builtin_nontemporal_load(q);
+  else
+    return *q;
+}
+__device__ __forceinline__ void store_words4(void* p, u32x4 v) {
+  u32x4_any* q = static_cast<u32x4_any*>(p);
+#if GASLOC_NONTEMPORAL
+  __builtin_nontemporal_store(v, q);
+#else
+  *q = v;
+#endif
+}
+__device__ __forceinline__ void store_words2(void* p, u32x2 v) {
+  u32x2_any* q = static_cast<u32x2_any*>(p);
+#if GASLOC_NONTEMPORAL
+  __builtin_nontemporal_store(v, q);
+#else
+  *q = v;
+#endif
+}
+
+template <int DT, int V, bool STREAM>
+__device__ __forceinline__ void load_row(const void* base, int64_t idx, int left, float (&o)[V]) {
+  static_assert(V == 4 || V == 8, "");
   if constexpr (DT == GASLOC_BF16) {
     const uint16_t* p = static_cast<const uint16_t*>(base) + idx;
-    if constexpr (V == 8) {
-      const u32x4 t = *reinterpret_cast<const u32x4*>(p);
+    if (left >= V) {
+      uint32_t t[V / 2];
+      if constexpr (V == 8) {
+        const u32x4 v = load_words4<STREAM>(p);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 4; ++k) t[k] = v[k];
+      } else {
+        const u32x2 v = load_words2<STREAM>(p);
+        t[0] = v.x;
+        t[1] = v.y;
+      }
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) {
         o[2 * k] = __uint_as_float(t[k] << 16);
         o[2 * k + 1] = __uint_as_float(t[k] & 0xffff0000u);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = bf16_to_f32(p[k]);
+      for (int k = 0; k < V; ++k) o[k] = k < left ? bf16_to_f32(p[k]) : 0.0f;
     }
   } else {
     const float* p = static_cast<const float*>(base) + idx;
-    if constexpr (V % 4 == 0) {
 #pragma unroll
-      for (int k = 0; k < V; k += 4) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(p + k);
+    for (int k = 0; k < V; k += 4) {
+      if (left >= k + 4) {
+        const f32x4 t = __builtin_bit_cast(f32x4, load_words4<STREAM>(p + k));
         o[k] = t.x; o[k + 1] = t.y; o[k + 2] = t.z; o[k + 3] = t.w;
+      } else {
+#pragma unroll
+        for (int e = k; e < k + 4; ++e) o[e] = e < left ? p[e] : 0.0f;
       }
+    }
+  }
+}
+
+template <int DT, int V>
+__device__ __forceinline__ void store_row(void* base, int64_t idx, int left, const float (&o)[V]) {
+  if constexpr (DT == GASLOC_BF16) {
+    uint16_t* p = static_cast<uint16_t*>(base) + idx;
+    uint32_t h[V / 2];
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) h[k] = f32x2_to_bf16x2(o[2 * k], o[2 * k + 1]);
+    if (left >= V) {
+      if constexpr (V == 8)
+        store_words4(p, u32x4{h[0], h[1], h[2], h[3]});
+      else
+        store_words2(p, u32x2{h[0], h[1]});
     } else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = p[k];
-    }
-  }
-}
-
-// The same with the streaming hint: data that is read once.
-template <int DT, int V>
-__device__ __forceinline__ void load_once(const void* base, int64_t idx, float (&o)[V]) {
-  if constexpr (DT == GASLOC_F32 && V == 8) {
-    float a[4], b[4];
-    load_f32<4>(static_cast<const float*>(base) + idx, 4, a);
-    load_f32<4>(static_cast<const float*>(base) + idx + 4, 4, b);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      o[k] = a[k];
-      o[4 + k] = b[k];
+      for (int k = 0; k < V; ++k)
+        if (k < left) p[k] = static_cast<uint16_t>(h[k / 2] >> (16 * (k & 1)));
     }
   } else {
-    load_params<DT, V>(base, idx, V, o);
-  }
-}
-
-template <int DT, int V>
-__device__ __forceinline__ void store_out(void* base, int64_t idx, const float (&o)[V]) {
-  if constexpr (DT == GASLOC_F32 && V == 8) {
-    float a[4], b[4];
+    float* p = static_cast<float*>(base) + idx;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      a[k] = o[k];
-      b[k] = o[4 + k];
+    for (int k = 0; k < V; k += 4) {
+      if (left >= k + 4) {
+        store_words4(p + k, __builtin_bit_cast(u32x4, f32x4{o[k], o[k + 1], o[k + 2], o[k + 3]}));
+      } else {
+#pragma unroll
+        for (int e = k; e < k + 4; ++e)
+          if (e < left) p[e] = o[e];
+      }
     }
-    store_f32<4>(static_cast<float*>(base) + idx, 4, a);
-    store_f32<4>(static_cast<float*>(base) + idx + 4, 4, b);
-  } else {
-    float kept[V];
-    store_params<DT, V>(base, idx, V, o, kept);
   }
 }
 

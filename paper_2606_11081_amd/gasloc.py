@@ -335,6 +335,12 @@ def gasloc_stream_probe(reads_f32, reads_bf16, writes_f32, writes_bf16, src, dst
     _check(st)
 
 
+def _row_ptr(a):
+    """row_ptr as (an int64 array that is kept alive, its address)."""
+    a = np.ascontiguousarray(a, dtype=np.int64)
+    return a, a.ctypes.data
+
+
 # Layers over the workers' rows (include/gasloc_layers.h).  row_ptr: n + 1 host numbers; activations, tokens,
 # gradients and workspaces: torch device tensors (or addresses).
 
@@ -348,7 +354,7 @@ def _act(dtype):
 
 
 def gasloc_embedding(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, out, out_ld):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_embedding(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
                                       _act(dtype), _dev(out), int(out_ld)), ctx)
     del keep
@@ -356,7 +362,7 @@ def gasloc_embedding(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, ou
 
 def gasloc_embedding_grad(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, dout, dout_ld, grads, grad_ld,
                           accumulate, workspace, workspace_bytes):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_embedding_grad(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
                                            _act(dtype), _dev(dout), int(dout_ld), _dev(grads), int(grad_ld),
                                            int(accumulate), _dev(workspace), int(workspace_bytes)), ctx)
@@ -364,7 +370,7 @@ def gasloc_embedding_grad(ctx, begin, vocab, width, scale, row_ptr, tokens, dtyp
 
 
 def gasloc_embedding_grad_workspace(ctx, width, row_ptr):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     out = ctypes.c_size_t()
     _check(library().gasloc_embedding_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
     del keep
@@ -372,7 +378,7 @@ def gasloc_embedding_grad_workspace(ctx, width, row_ptr):
 
 
 def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out, out_ld, stats=None):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_layer_norm(ctx, int(gain), int(bias), int(width), float(eps), rp, _dev(x), int(x_ld),
                                        _act(dtype), _dev(out), int(out_ld), _dev(stats)), ctx)
     del keep
@@ -380,7 +386,7 @@ def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out,
 
 def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout, dout_ld, dtype, dx, dx_ld, grads,
                            grad_ld, accumulate, workspace, workspace_bytes):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_layer_norm_grad(ctx, int(gain), int(bias), int(width), rp, _dev(x), int(x_ld),
                                             _dev(stats), _dev(dout), int(dout_ld), _act(dtype), _dev(dx), int(dx_ld),
                                             _dev(grads), int(grad_ld), int(accumulate), _dev(workspace),
@@ -389,7 +395,7 @@ def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout
 
 
 def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     out = ctypes.c_size_t()
     _check(library().gasloc_layer_norm_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
     del keep
@@ -397,14 +403,14 @@ def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
 
 
 def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtype, out, out_ld):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_linear(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x), int(x_ld),
                                    _act(dtype), _dev(out), int(out_ld)), ctx)
     del keep
 
 
 def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, dout, dout_ld, dtype, dx, dx_ld):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_linear_grad_input(ctx, int(weight), int(out_features), int(in_features), rp, _dev(dout),
                                               int(dout_ld), _act(dtype), _dev(dx), int(dx_ld)), ctx)
     del keep
@@ -412,7 +418,7 @@ def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, do
 
 def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dout, dout_ld, dtype, grads,
                               grad_ld, accumulate, workspace, workspace_bytes):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_linear_grad_weight(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x),
                                                int(x_ld), _dev(dout), int(dout_ld), _act(dtype), _dev(grads),
                                                int(grad_ld), int(accumulate), _dev(workspace),
@@ -421,7 +427,7 @@ def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x
 
 
 def gasloc_linear_grad_weight_workspace(ctx, out_features, in_features, row_ptr):
-    keep, rp = _host(row_ptr, np.int64)
+    keep, rp = _row_ptr(row_ptr)
     out = ctypes.c_size_t()
     _check(library().gasloc_linear_grad_weight_workspace(ctx, int(out_features), int(in_features), rp,
                                                          ctypes.byref(out)))
@@ -475,38 +481,18 @@ def alloc_buffers(n, P, param_dtype="f32", device="cuda", with_u=True, with_zp=T
 
 
 def _rows_of(name, t, rows, cols, dtype, device):
-    """Checks that tensor t can hold (at least) `rows` rows of `cols` elements, each contiguous; returns its row length."""
+    """Checks that tensor t holds (at least) `rows` rows of `cols` elements, each contiguous; returns its row length."""
+    shape = t.shape
     if t.dtype != dtype or t.device != device:
         raise ValueError("%s must be %s on %s, not %s on %s" % (name, dtype, device, t.dtype, t.device))
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or \
-            (t.numel() > 0 and cols > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be at least %d rows of %d contiguous elements, not %s with strides %s"
-                         % (name, rows, cols, tuple(t.shape), tuple(t.stride())))
-    return t.stride(0) if t.shape[0] > 1 else cols  # the stride of a single row means nothing
-
-
-class _OnStream:
-    """Runs a call on the context's stream between the current stream's work: what the current
-    stream has enqueued is seen by the call, and what it enqueues next sees the results."""
-
-    def __init__(self, stream, tensors):
-        self.stream, self.tensors = stream, tensors
-
-    def __enter__(self):
-        import torch
-
-        self.current = torch.cuda.current_stream(self.stream.device)
-        self.other = self.current.cuda_stream != self.stream.cuda_stream
-        if self.other:
-            self.stream.wait_stream(self.current)
-            for t in self.tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
-
-    def __exit__(self, *exc):
-        if self.other:
-            self.current.wait_stream(self.stream)
-        return False
+    if len(shape) == 2 and shape[0] >= rows and shape[1] == cols:
+        if shape[0] == 0 or cols == 0:
+            return cols
+        ld, step = t.stride()
+        if step == 1 or cols == 1:
+            return ld if shape[0] > 1 else cols  # the stride of a single row means nothing
+    raise ValueError("%s must be at least %d rows of %d contiguous elements, not %s with strides %s"
+                     % (name, rows, cols, tuple(shape), tuple(t.stride())))
 
 
 class GASLoC:
@@ -577,18 +563,36 @@ class GASLoC:
             raise ValueError("row_ptr needs %d numbers" % (self.n + 1))
         return rp, int(rp[-1]), self.bufs["x"].device
 
-    def _new(self, t, rows, cols, dtype):
+    def _run(self, call, tensors, *args):
+        """A call on the context's stream, in order with the current one: it sees what the current stream has
+        enqueued, and what that enqueues next sees the results."""
         import torch
 
-        return torch.empty((rows, cols), dtype=dtype, device=self.bufs["x"].device) if t is None else t
+        current = torch.cuda.current_stream(self.stream.device)
+        if current.cuda_stream == self.stream.cuda_stream:
+            call(self.ctx, *args)
+            return
+        self.stream.wait_stream(current)
+        for t in tensors:
+            t.record_stream(self.stream)
+        call(self.ctx, *args)
+        current.wait_stream(self.stream)
 
-    def _workspace(self, workspace, need):
+    def _out(self, name, t, rows, cols, dtype, device):
+        """The tensor a result goes to (a new one for None) and its row length."""
+        import torch
+
+        if t is None:
+            return torch.empty((rows, cols), dtype=dtype, device=device), cols
+        return t, _rows_of(name, t, rows, cols, dtype, device)
+
+    def _workspace(self, workspace, need, device):
         import torch
 
         if workspace is None:
-            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=self.bufs["x"].device)
-        if workspace.device != self.bufs["x"].device or not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous on %s" % self.bufs["x"].device)
+            return torch.empty(need, dtype=torch.uint8, device=device), need
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous on %s" % device)
         return workspace, workspace.numel() * workspace.element_size()
 
     def _tokens(self, tokens, rows, device):
@@ -606,21 +610,24 @@ class GASLoC:
         ld = _rows_of("grads", grads, self.n, grads.shape[1], torch.float32, device)
         return ld if self.n > 1 else (ld + 3) // 4 * 4
 
+    def _stats(self, stats, rows, device):
+        import torch
+
+        stats, ld = self._out("stats", stats, rows, 2, torch.float32, device)
+        if ld != 2:
+            raise ValueError("stats must be contiguous")
+        return stats
+
     def embedding(self, table, vocab, width, tokens, row_ptr, scale=1.0, dtype=None, out=None):
         """out[t] = scale * E_i[tokens[t]], E_i the [vocab, width] table at column `table` of worker i's row;
         tokens outside the table give zeros.  dtype: "f32" or "bf16" (that of out; default: the parameters')."""
         import torch
 
         rp, rows, device = self._layer(row_ptr)
-        if out is not None:
-            dt = out.dtype
-        else:
-            dt = torch.bfloat16 if _act(self.bufs["x"].dtype if dtype is None else dtype) == GASLOC_BF16 else torch.float32
-        out = self._new(out, rows, width, dt)
-        ld = _rows_of("out", out, rows, width, dt, device)
+        code = _act(out.dtype if out is not None else self.bufs["x"].dtype if dtype is None else dtype)
+        out, ld = self._out("out", out, rows, width, torch.bfloat16 if code == GASLOC_BF16 else torch.float32, device)
         self._tokens(tokens, rows, device)
-        with _OnStream(self.stream, (tokens, out)):
-            gasloc_embedding(self.ctx, table, vocab, width, scale, rp, tokens, dt, out, ld)
+        self._run(gasloc_embedding, (tokens, out), table, vocab, width, scale, rp, tokens, code, out, ld)
         return out
 
     def embedding_grad(self, table, vocab, width, tokens, row_ptr, dout, grads, scale=1.0, accumulate=False,
@@ -630,33 +637,20 @@ class GASLoC:
         ld = _rows_of("dout", dout, rows, width, dout.dtype, device)
         gld = self._grads(grads, device)
         self._tokens(tokens, rows, device)
-        ws, size = self._workspace(workspace, gasloc_embedding_grad_workspace(self.ctx, width, rp))
-        with _OnStream(self.stream, (tokens, dout, grads, ws)):
-            gasloc_embedding_grad(self.ctx, table, vocab, width, scale, rp, tokens, dout.dtype, dout, ld, grads, gld,
-                                  bool(accumulate), ws, size)
+        ws, size = self._workspace(workspace, gasloc_embedding_grad_workspace(self.ctx, width, rp), device)
+        self._run(gasloc_embedding_grad, (tokens, dout, grads, ws), table, vocab, width, scale, rp, tokens, dout.dtype,
+                  dout, ld, grads, gld, bool(accumulate), ws, size)
 
     def layer_norm(self, gain, bias, width, x, row_ptr, eps=1e-5, out=None, stats=None):
         """(out, stats): the normalised rows (gain and bias at these columns; bias None: none) and every
         row's (mean, rstd) for layer_norm_grad.  out may be x."""
-        import torch
-
         rp, rows, device = self._layer(row_ptr)
         x_ld = _rows_of("x", x, rows, width, x.dtype, device)
-        out = self._new(out, rows, width, x.dtype)
-        ld = _rows_of("out", out, rows, width, x.dtype, device)
+        out, ld = self._out("out", out, rows, width, x.dtype, device)
         stats = self._stats(stats, rows, device)
-        with _OnStream(self.stream, (x, out, stats)):
-            gasloc_layer_norm(self.ctx, gain, -1 if bias is None else bias, width, eps, rp, x, x_ld, x.dtype, out, ld,
-                              stats)
+        self._run(gasloc_layer_norm, (x, out, stats), gain, -1 if bias is None else bias, width, eps, rp, x, x_ld,
+                  x.dtype, out, ld, stats)
         return out, stats
-
-    def _stats(self, stats, rows, device):
-        import torch
-
-        stats = self._new(stats, rows, 2, torch.float32)
-        if _rows_of("stats", stats, rows, 2, torch.float32, device) != 2 and rows > 1:
-            raise ValueError("stats must be contiguous")
-        return stats
 
     def layer_norm_grad(self, gain, bias, width, x, row_ptr, stats, dout, grads, dx=None, accumulate=False,
                         workspace=None):
@@ -665,34 +659,31 @@ class GASLoC:
         rp, rows, device = self._layer(row_ptr)
         x_ld = _rows_of("x", x, rows, width, x.dtype, device)
         d_ld = _rows_of("dout", dout, rows, width, x.dtype, device)
-        dx = self._new(dx, rows, width, x.dtype)
-        ld = _rows_of("dx", dx, rows, width, x.dtype, device)
+        dx, ld = self._out("dx", dx, rows, width, x.dtype, device)
+        if stats is None:
+            raise ValueError("stats: those that layer_norm returned")
         stats = self._stats(stats, rows, device)
         gld = self._grads(grads, device)
-        ws, size = self._workspace(workspace, gasloc_layer_norm_grad_workspace(self.ctx, width, rp))
-        with _OnStream(self.stream, (x, stats, dout, dx, grads, ws)):
-            gasloc_layer_norm_grad(self.ctx, gain, -1 if bias is None else bias, width, rp, x, x_ld, stats, dout, d_ld,
-                                   x.dtype, dx, ld, grads, gld, bool(accumulate), ws, size)
+        ws, size = self._workspace(workspace, gasloc_layer_norm_grad_workspace(self.ctx, width, rp), device)
+        self._run(gasloc_layer_norm_grad, (x, stats, dout, dx, grads, ws), gain, -1 if bias is None else bias, width,
+                  rp, x, x_ld, stats, dout, d_ld, x.dtype, dx, ld, grads, gld, bool(accumulate), ws, size)
         return dx
 
     def linear(self, weight, out_features, in_features, x, row_ptr, out=None):
         """out[t] = W_i x[t], W_i the [out_features, in_features] matrix at column `weight` of worker i's row."""
         rp, rows, device = self._layer(row_ptr)
         x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
-        out = self._new(out, rows, out_features, x.dtype)
-        ld = _rows_of("out", out, rows, out_features, x.dtype, device)
-        with _OnStream(self.stream, (x, out)):
-            gasloc_linear(self.ctx, weight, out_features, in_features, rp, x, x_ld, x.dtype, out, ld)
+        out, ld = self._out("out", out, rows, out_features, x.dtype, device)
+        self._run(gasloc_linear, (x, out), weight, out_features, in_features, rp, x, x_ld, x.dtype, out, ld)
         return out
 
     def linear_grad_input(self, weight, out_features, in_features, dout, row_ptr, dx=None):
         """dx[t] = W_i^T dout[t]."""
         rp, rows, device = self._layer(row_ptr)
         d_ld = _rows_of("dout", dout, rows, out_features, dout.dtype, device)
-        dx = self._new(dx, rows, in_features, dout.dtype)
-        ld = _rows_of("dx", dx, rows, in_features, dout.dtype, device)
-        with _OnStream(self.stream, (dout, dx)):
-            gasloc_linear_grad_input(self.ctx, weight, out_features, in_features, rp, dout, d_ld, dout.dtype, dx, ld)
+        dx, ld = self._out("dx", dx, rows, in_features, dout.dtype, device)
+        self._run(gasloc_linear_grad_input, (dout, dx), weight, out_features, in_features, rp, dout, d_ld, dout.dtype,
+                  dx, ld)
         return dx
 
     def linear_grad_weight(self, weight, out_features, in_features, x, dout, row_ptr, grads, accumulate=False,
@@ -703,10 +694,9 @@ class GASLoC:
         d_ld = _rows_of("dout", dout, rows, out_features, x.dtype, device)
         gld = self._grads(grads, device)
         ws, size = self._workspace(
-            workspace, gasloc_linear_grad_weight_workspace(self.ctx, out_features, in_features, rp))
-        with _OnStream(self.stream, (x, dout, grads, ws)):
-            gasloc_linear_grad_weight(self.ctx, weight, out_features, in_features, rp, x, x_ld, dout, d_ld, x.dtype,
-                                      grads, gld, bool(accumulate), ws, size)
+            workspace, gasloc_linear_grad_weight_workspace(self.ctx, out_features, in_features, rp), device)
+        self._run(gasloc_linear_grad_weight, (x, dout, grads, ws), weight, out_features, in_features, rp, x, x_ld,
+                  dout, d_ld, x.dtype, grads, gld, bool(accumulate), ws, size)
 
     def counters(self):
         """(k, stepped, rounds_done): per-worker AdamW step counts, which workers
