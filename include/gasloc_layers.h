@@ -112,29 +112,31 @@ gasloc_status gasloc_layer_norm_grad_workspace(const gasloc_ctx *ctx, int32_t wi
 /* Linear layer without bias: out[t, :] = W_i x[t, :] for every row t of worker
  * i; W_i: [out_features, in_features] at column `weight`.  F32 weights meet
  * BF16 activations rounded to BF16 (nearest even), as in a mixed-precision
- * step.  Features in [1, 2^20].  Enqueues one kernel. */
+ * step.  Features in [1, 2^20].  Enqueues one kernel, and one more where a
+ * product with few rows is split along its sums.  workspace: at least
+ * gasloc_linear_workspace bytes (may be NULL if that is 0). */
 gasloc_status gasloc_linear(gasloc_ctx *ctx, int64_t weight, int32_t out_features, int32_t in_features,
                             const int64_t *row_ptr, const void *x, int64_t x_ld, int32_t dtype, void *out,
-                            int64_t out_ld);
+                            int64_t out_ld, void *workspace, size_t workspace_bytes);
 
-/* Its gradient of the input, dx[t, :] = W_i^T dout[t, :]; weights rounded as in
- * the forward pass.  Enqueues one kernel. */
+/* Its gradient of the input, dx[t, :] = W_i^T dout[t, :]; weights rounded, kernels
+ * and workspace as in the forward pass. */
 gasloc_status gasloc_linear_grad_input(gasloc_ctx *ctx, int64_t weight, int32_t out_features, int32_t in_features,
                                        const int64_t *row_ptr, const void *dout, int64_t dout_ld, int32_t dtype,
-                                       void *dx, int64_t dx_ld);
+                                       void *dx, int64_t dx_ld, void *workspace, size_t workspace_bytes);
 
 /* Its gradient of the weight, grads_i[weight + o * in_features + c] (+)= sum_t
- * dout[t, o] * x[t, c] over the rows of worker i.  Enqueues one kernel, and one
- * more where the rows are split.  workspace: at least
- * gasloc_linear_grad_weight_workspace bytes (may be 0). */
+ * dout[t, o] * x[t, c] over the rows of worker i.  Kernels and workspace as
+ * in the forward pass. */
 gasloc_status gasloc_linear_grad_weight(gasloc_ctx *ctx, int64_t weight, int32_t out_features, int32_t in_features,
                                         const int64_t *row_ptr, const void *x, int64_t x_ld, const void *dout,
                                         int64_t dout_ld, int32_t dtype, float *grads, int64_t grad_ld,
                                         int32_t accumulate, void *workspace, size_t workspace_bytes);
 
-/* Bytes of workspace for gasloc_linear_grad_weight with these rows.  Host only. */
-gasloc_status gasloc_linear_grad_weight_workspace(const gasloc_ctx *ctx, int32_t out_features, int32_t in_features,
-                                                  const int64_t *row_ptr, size_t *bytes);
+/* Bytes of workspace with which each of the three calls can be made for a
+ * layer of these sizes with these rows.  Host only. */
+gasloc_status gasloc_linear_workspace(const gasloc_ctx *ctx, int32_t out_features, int32_t in_features,
+                                      const int64_t *row_ptr, int32_t dtype, size_t *bytes);
 
 #ifdef __cplusplus
 }

@@ -146,10 +146,20 @@ struct LinearArgs {
   float* grads;  // weight
   int64_t grad_ld;
   int32_t accumulate;
-  Spans rows, tiles;
-  uint8_t order[kMaxReplicas];  // weight: the worker of each span of tiles
+  Spans rows;
+  Spans tiles;                  // workgroups of each span (a worker's), all parts of k
+  uint8_t order[kMaxReplicas];  // weight: the worker of each span
+  // A product with few tiles is split along k into parts of `chunk` (0: not split); parts.begin counts the parts of
+  // the spans before (weight; else all spans have the same number of parts).  partial: the parts' fp32 sums, one
+  // matrix per part (weight), or one set of all rows per part.
+  int32_t chunk;
+  Spans parts;
+  float* partial;
 };
-// tile: rows and columns of a workgroup's part of C (256, or 128: always 128 without vec and in F32); vec: every row of either operand, of C and of
+constexpr int kLinearStep = 64;  // bytes of k per step; the kernel takes four at a time
+constexpr int kFewRows = 16;
+// tile: rows and columns of a workgroup's part of C (256, or 128: always 128 without vec and in F32; kFewRows:
+// forward pass of workers with at most so many rows, 16 outputs of all of them per workgroup); vec: every row of either operand, of C and of
 // the gradients begins on a 16-byte boundary and is a whole number of 16-byte chunks of activations.
 hipError_t launch_linear(const LinearArgs& a, LinearPass pass, int params, int act, int tile, bool vec,
                          hipStream_t stream);

@@ -125,18 +125,28 @@ struct Operand {
 #pragma unroll
       for (int e = 0; e < 4; ++e) words[j][e] = v[e];
     } else {
-      const bool inside = line_of(j) < l.lines;
-      uint32_t e[E];
+      // Whole chunks at the alignment of an element, which the memory instructions take; the one that goes over the
+      // end of a line by elements.
+      const bool in_line = line_of(j) < l.lines;
+      const uint32_t o = off + down;
+      const u32x4 v = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.w, in_line && col + E <= l.limit ? o : kNowhere, 0, 0));
 #pragma unroll
-      for (int q = 0; q < E; ++q) {
-        const uint32_t o = inside && col + q < l.limit ? off + down + q * kSrc : kNowhere;
-        if constexpr (ST == GASLOC_BF16)
-          e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(l.w, o, 0, 0));
-        else
-          e[q] = __builtin_amdgcn_raw_buffer_load_b32(l.w, o, 0, 0);
+      for (int e = 0; e < 4; ++e) words[j][e] = v[e];
+      if (in_line && col < l.limit && col + E > l.limit) {
+        uint32_t e[E];
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+          const uint32_t at_q = col + q < l.limit ? o + q * kSrc : kNowhere;
+          if constexpr (ST == GASLOC_BF16)
+            e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(l.w, at_q, 0, 0));
+          else
+            e[q] = __builtin_amdgcn_raw_buffer_load_b32(l.w, at_q, 0, 0);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          words[j][q] = ST == GASLOC_BF16 ? e[2 * q % E] | e[(2 * q + 1) % E] << 16 : e[q % E];
       }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) words[j][q] = ST == GASLOC_BF16 ? e[2 * q % E] | e[(2 * q + 1) % E] << 16 : e[q % E];
     }
   }
   // Where chunk 0 of this thread goes, and the lane's part of the fragment that begins at row `row` of the tile.
@@ -208,8 +218,9 @@ __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c) {
   }
 }
 
-// A tile of TM x TN outputs by WAVES_M x WAVES_N waves.
-template <int PASS, int PT, int AT, int TM, int TN, int WAVES_M, int WAVES_N, bool VEC>
+// A tile of TM x TN outputs by WAVES_M x WAVES_N waves.  SPLIT: a workgroup takes `chunk` of k, and where a worker
+// has several such parts it leaves its sums in `partial` for the join.
+template <int PASS, int PT, int AT, int TM, int TN, int WAVES_M, int WAVES_N, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a) {
   constexpr int THREADS = kWave * WAVES_M * WAVES_N;
   constexpr bool kForward = PASS == kLinearForward, kWeight = PASS == kLinearWeight;
@@ -233,13 +244,18 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   const int t = from + xcd * each + (xcd < more ? xcd : more) + (b - from) / 8;
   const int span = kWeight ? owner : find_worker(a.tiles, a.n, t);
   const int i = kWeight ? a.order[span] : span;
-  const int tile = t - a.tiles.begin[span];
   const int64_t r0 = a.rows.begin[i];
   const int count = a.rows.begin[i + 1] - a.rows.begin[i];
   const int M = kWeight ? a.out_features : count;
   const int N = kForward ? a.out_features : a.in_features;
-  const int depth = kForward ? a.in_features : kWeight ? count : a.out_features;
+  const int whole = kForward ? a.in_features : kWeight ? count : a.out_features;
   const int across = (N + TN - 1) / TN;
+  // parts of k: first all tiles of the first part
+  const int tiles = across * ((M + TM - 1) / TM);
+  const int part = SPLIT ? (t - a.tiles.begin[span]) / tiles : 0;
+  const int tile = t - a.tiles.begin[span] - part * tiles;
+  const int k_first = SPLIT ? part * a.chunk : 0;
+  const int depth = SPLIT ? min(whole - k_first, a.chunk) : whole;
   // kGroup tiles of m by all of n at a time, m first: the tiles that an XCD works on at once are about as many of m as
   // of n, which is what has to be read least for.
   constexpr int kGroup = TM == 256 ? 4 : 8;
@@ -252,14 +268,14 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   OpA oa;
   OpB ob;
   if constexpr (kForward) {
-    oa.start(static_cast<const char*>(a.x) + (r0 + m0) * a.x_ld * kAct, a.x_ld, M - m0, depth);
-    ob.start(w + static_cast<int64_t>(n0) * depth * kPar, depth, N - n0, depth);
+    oa.start(static_cast<const char*>(a.x) + ((r0 + m0) * a.x_ld + k_first) * kAct, a.x_ld, M - m0, depth);
+    ob.start(w + (static_cast<int64_t>(n0) * whole + k_first) * kPar, whole, N - n0, depth);
   } else if constexpr (!kWeight) {
-    oa.start(static_cast<const char*>(a.dout) + (r0 + m0) * a.dout_ld * kAct, a.dout_ld, M - m0, depth);
-    ob.start(w + static_cast<int64_t>(n0) * kPar, N, N - n0, depth);
+    oa.start(static_cast<const char*>(a.dout) + ((r0 + m0) * a.dout_ld + k_first) * kAct, a.dout_ld, M - m0, depth);
+    ob.start(w + (static_cast<int64_t>(k_first) * N + n0) * kPar, N, N - n0, depth);
   } else {
-    oa.start(static_cast<const char*>(a.dout) + (r0 * a.dout_ld + m0) * kAct, a.dout_ld, M - m0, depth);
-    ob.start(static_cast<const char*>(a.x) + (r0 * a.x_ld + n0) * kAct, a.x_ld, N - n0, depth);
+    oa.start(static_cast<const char*>(a.dout) + ((r0 + k_first) * a.dout_ld + m0) * kAct, a.dout_ld, M - m0, depth);
+    ob.start(static_cast<const char*>(a.x) + ((r0 + k_first) * a.x_ld + n0) * kAct, a.x_ld, N - n0, depth);
   }
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -366,15 +382,28 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
 
   // Lane l holds row l % 16 and columns 4 (l / 16) .. + 3 of each 16 x 16 block.  Sixteen rows at a time go
   // through the wave's own part of LDS, so that whole lines are stored.
-  using Out = typename std::conditional<kWeight || AT == GASLOC_F32, float, uint16_t>::type;
+  using Out = typename std::conditional<kWeight || AT == GASLOC_F32 || SPLIT, float, uint16_t>::type;
   constexpr int kOutStride = WN * static_cast<int>(sizeof(Out)) + 16;
   constexpr int V = VEC ? 16 / static_cast<int>(sizeof(Out)) : 1;
   static_assert(THREADS / kWave * 16 * kOutStride <= kBuffers * (OpA::kLds + OpB::kLds), "sixteen rows of every wave fit");
   char* const mine = s_tiles + wave * 16 * kOutStride;
   const int lane = lane_id();
-  Out* const out = kWeight ? reinterpret_cast<Out*>(a.grads + static_cast<int64_t>(i) * a.grad_ld + a.weight)
-                           : static_cast<Out*>(a.out) + r0 * a.out_ld;
-  const int64_t out_ld = kWeight ? N : a.out_ld;
+  Out* out;
+  int64_t out_ld = kWeight ? N : a.out_ld;
+  const bool split = SPLIT && a.parts.begin[span + 1] - a.parts.begin[span] > 1;
+  bool add = false;
+  if (split) {
+    // weight: one matrix per part of every worker; else one set of all rows per part
+    const int64_t at = kWeight ? static_cast<int64_t>(a.parts.begin[span] + part) * M * N
+                               : (static_cast<int64_t>(part) * a.rows.begin[a.n] + r0) * N;
+    out = reinterpret_cast<Out*>(a.partial + at);
+    out_ld = N;
+  } else if constexpr (kWeight) {
+    out = a.grads + static_cast<int64_t>(i) * a.grad_ld + a.weight;
+    add = a.accumulate;
+  } else {
+    out = static_cast<Out*>(a.out) + r0 * a.out_ld;
+  }
 #pragma unroll
   for (int p = 0; p < FM; ++p) {
     __builtin_amdgcn_wave_barrier();
@@ -398,14 +427,14 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
       Out* to = out + (top + row) * out_ld + n;
       if constexpr (VEC && kWeight) {
         f32x4 v = *reinterpret_cast<const f32x4*>(from);
-        if (a.accumulate) v += *reinterpret_cast<const f32x4*>(to);
+        if (add) v += *reinterpret_cast<const f32x4*>(to);
         *reinterpret_cast<f32x4*>(to) = v;
       } else if constexpr (VEC) {
         *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(from);
       } else {
         const Out v = *reinterpret_cast<const Out*>(from);
         if constexpr (kWeight)
-          *to = a.accumulate ? *to + v : v;
+          *to = add ? *to + v : v;
         else
           *to = v;
       }
@@ -414,14 +443,134 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   }
 }
 
+// Adds the parts of a split product in order and stores the sums: for the weight's gradient those of the worker of
+// span blockIdx.y (if it has more than one part), else all rows.
+template <int PASS, int AT>
+__global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
+  constexpr bool kWeight = PASS == kLinearWeight;
+  const int span = blockIdx.y;
+  const int parts = a.parts.begin[span + 1] - a.parts.begin[span];
+  if (kWeight && parts < 2) return;
+  const int N = PASS == kLinearForward ? a.out_features : a.in_features;
+  const int64_t all = static_cast<int64_t>(kWeight ? a.out_features : a.rows.begin[a.n]) * N;
+  const float* p = a.partial + (kWeight ? a.parts.begin[span] * all : 0);
+  for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < all; e += gridDim.x * 256ll) {
+    float sum = p[e];
+#pragma unroll 4
+    for (int k = 1; k < parts; ++k) sum += p[k * all + e];
+    if constexpr (kWeight) {
+      float* to = a.grads + static_cast<int64_t>(a.order[span]) * a.grad_ld + a.weight + e;
+      *to = a.accumulate ? *to + sum : sum;
+    } else {
+      const int64_t at = e / N * a.out_ld + e % N;
+      if constexpr (AT == GASLOC_BF16)
+        static_cast<uint16_t*>(a.out)[at] = static_cast<uint16_t>(f32x2_to_bf16x2(sum, 0.0f) & 0xffffu);
+      else
+        static_cast<float*>(a.out)[at] = sum;
+    }
+  }
+}
+
+// Forward pass of workers with at most kFewRows rows each: reading the weights is all there is to it, so they go from
+// memory to the matrix cores through registers, 16 outputs per workgroup, each of its four waves a quarter of k.
+// Lane l has output l % 16 of the weights and row l % 16 of x.  bf16 weights: of every 32 of k the 8 from 8 (l / 16) on;
+// fp32 ones: the 4 from 4 (l / 16) on and the 4 that lie 16 behind them.  Either way a load takes 64 bytes of 16 rows,
+// and the other half of those lines is next, so the loads go through the caches.
+template <int PT, int AT>
+__global__ __launch_bounds__(256) void k_linear_rows(LinearArgs a) {
+  constexpr int kAhead = 4;                        // 32s of k in flight
+  constexpr int V = PT == GASLOC_BF16 ? 8 : 4;     // of k per load
+  constexpr int H = 8 / V;
+  __shared__ f32x4 s_sum[4][kWave];
+  const int i = find_worker(a.tiles, a.n, blockIdx.x);
+  const int64_t r0 = a.rows.begin[i];
+  const int rows = a.rows.begin[i + 1] - a.rows.begin[i];
+  const int N = a.out_features, K = a.in_features;
+  const int n0 = (static_cast<int>(blockIdx.x) - a.tiles.begin[i]) * 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int quarter = (K + 4 * 32 - 1) / (4 * 32) * 32;
+  const int k_first = wave * quarter, k_end = min(K, k_first + quarter);
+  const int mine = n0 + lane % 16;
+  const int64_t w_at = a.weight + static_cast<int64_t>(mine < N ? mine : N - 1) * K;
+  const int64_t x_at = (r0 + (lane % 16 < rows ? lane % 16 : 0)) * a.x_ld;
+  const bool has_row = lane % 16 < rows;
+  const void* w = live_row<PT>(a.w, i);
+  f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+  // WHOLE: all of the block lies inside, so that its loads are issued back to back
+  const auto block = [&](int k_block, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
+    constexpr int kDeep = kWhole ? kAhead : 1;
+    float fw[kDeep][8], fx[kDeep][8];
+#pragma unroll
+    for (int q = 0; q < kDeep; ++q) {
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const int k = k_block + lane / 16 * V + 32 * q + 16 * h, left = kWhole ? V : max(0, k_end - k);
+        float pw[V], px[V];
+        load_row<PT, V, false>(w, w_at + k, left, pw);
+        load_row<AT, V, false>(a.x, x_at + k, left, px);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          fw[q][h * V + e] = pw[e];
+          fx[q][h * V + e] = px[e];
+        }
+      }
+    }
+    if (kWhole) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < kDeep; ++q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) fx[q][e] = has_row ? fx[q][e] : 0.0f;
+      if constexpr (AT == GASLOC_BF16) {
+        u32x4 fa, fb;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          fa[e] = f32x2_to_bf16x2(fw[q][2 * e], fw[q][2 * e + 1]);
+          fb[e] = f32x2_to_bf16x2(fx[q][2 * e], fx[q][2 * e + 1]);
+        }
+        c = multiply<AT>(fa, fb, c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[q][e], fx[q][e], c, 0, 0, 0);
+      }
+    }
+  };
+  int k = k_first;
+  for (; k + 32 * kAhead <= k_end; k += 32 * kAhead) block(k, std::true_type{});
+  for (; k < k_end; k += 32) block(k, std::false_type{});
+  s_sum[wave][lane] = c;
+  __syncthreads();
+  if (wave != 0 || !has_row) return;
+#pragma unroll
+  for (int k = 1; k < 4; ++k) c += s_sum[k][lane];
+  // the lane holds outputs n0 + 4 (l / 16) .. + 3 of row l % 16
+  const int n = n0 + lane / 16 * 4;
+  const float o[4] = {c[0], c[1], c[2], c[3]};
+  if (n < N) store_row<AT, 4>(a.out, (r0 + lane % 16) * a.out_ld + n, N - n, o);
+}
+
 template <int PASS, int PT, int AT>
 hipError_t launch_types(const LinearArgs& a, int tile, bool vec, hipStream_t stream) {
   const dim3 grid(a.tiles.begin[a.n]);
   if constexpr (AT == GASLOC_BF16) {
-    if (tile == 256) return launch_kernel(k_linear<PASS, PT, AT, 256, 256, 2, 4, true>, grid, 512, 0, stream, a);
+    if (tile == 256)
+      return launch_kernel(k_linear<PASS, PT, AT, 256, 256, 2, 4, true, false>, grid, 512, 0, stream, a);
   }
-  return launch_kernel(vec ? k_linear<PASS, PT, AT, 128, 128, 2, 2, true> : k_linear<PASS, PT, AT, 128, 128, 2, 2, false>,
-                       grid, 256, 0, stream, a);
+  if constexpr (PASS == kLinearForward) {
+    if (tile == kFewRows) return launch_kernel(k_linear_rows<PT, AT>, grid, 256, 0, stream, a);
+  }
+  if (a.chunk == 0)
+    return launch_kernel(vec ? k_linear<PASS, PT, AT, 128, 128, 2, 2, true, false>
+                             : k_linear<PASS, PT, AT, 128, 128, 2, 2, false, false>,
+                         grid, 256, 0, stream, a);
+  const hipError_t e = launch_kernel(vec ? k_linear<PASS, PT, AT, 128, 128, 2, 2, true, true>
+                                         : k_linear<PASS, PT, AT, 128, 128, 2, 2, false, true>,
+                                     grid, 256, 0, stream, a);
+  if (e != hipSuccess) return e;
+  const int N = PASS == kLinearForward ? a.out_features : a.in_features;
+  const int64_t all = static_cast<int64_t>(PASS == kLinearWeight ? a.out_features : a.rows.begin[a.n]) * N;
+  const dim3 join(static_cast<unsigned>(all / 256 < 2048 ? (all + 255) / 256 : 2048), PASS == kLinearWeight ? a.n : 1);
+  return launch_kernel(k_linear_join<PASS, AT>, join, 256, 0, stream, a);
 }
 
 template <int PASS>

@@ -94,11 +94,12 @@ _SIGNATURES = {
     "gasloc_layer_norm_grad": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _i64,
                                               _vp, _i64, _i32, _vp, ctypes.c_size_t]),
     "gasloc_layer_norm_grad_workspace": (ctypes.c_int, [_vp, _i32, _vp, ctypes.POINTER(ctypes.c_size_t)]),
-    "gasloc_linear": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i64]),
-    "gasloc_linear_grad_input": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i64]),
+    "gasloc_linear": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i64, _vp, ctypes.c_size_t]),
+    "gasloc_linear_grad_input": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _i32, _vp, _i64, _vp,
+                                                ctypes.c_size_t]),
     "gasloc_linear_grad_weight": (ctypes.c_int, [_vp, _i64, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _i32, _vp, _i64,
                                                  _i32, _vp, ctypes.c_size_t]),
-    "gasloc_linear_grad_weight_workspace": (ctypes.c_int, [_vp, _i32, _i32, _vp, ctypes.POINTER(ctypes.c_size_t)]),
+    "gasloc_linear_workspace": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, ctypes.POINTER(ctypes.c_size_t)]),
     "gasloc_last_error": (ctypes.c_char_p, [_vp]),
     "gasloc_build_info": (ctypes.c_char_p, []),
     "gasloc_destroy": (None, [_vp]),
@@ -402,17 +403,20 @@ def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
     return out.value
 
 
-def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtype, out, out_ld):
+def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtype, out, out_ld, workspace=None,
+                  workspace_bytes=0):
     keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_linear(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x), int(x_ld),
-                                   _act(dtype), _dev(out), int(out_ld)), ctx)
+                                   _act(dtype), _dev(out), int(out_ld), _dev(workspace), int(workspace_bytes)), ctx)
     del keep
 
 
-def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, dout, dout_ld, dtype, dx, dx_ld):
+def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, dout, dout_ld, dtype, dx, dx_ld,
+                             workspace=None, workspace_bytes=0):
     keep, rp = _row_ptr(row_ptr)
     _check(library().gasloc_linear_grad_input(ctx, int(weight), int(out_features), int(in_features), rp, _dev(dout),
-                                              int(dout_ld), _act(dtype), _dev(dx), int(dx_ld)), ctx)
+                                              int(dout_ld), _act(dtype), _dev(dx), int(dx_ld), _dev(workspace),
+                                              int(workspace_bytes)), ctx)
     del keep
 
 
@@ -426,11 +430,11 @@ def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x
     del keep
 
 
-def gasloc_linear_grad_weight_workspace(ctx, out_features, in_features, row_ptr):
+def gasloc_linear_workspace(ctx, out_features, in_features, row_ptr, dtype):
     keep, rp = _row_ptr(row_ptr)
     out = ctypes.c_size_t()
-    _check(library().gasloc_linear_grad_weight_workspace(ctx, int(out_features), int(in_features), rp,
-                                                         ctypes.byref(out)))
+    _check(library().gasloc_linear_workspace(ctx, int(out_features), int(in_features), rp, _act(dtype),
+                                             ctypes.byref(out)))
     del keep
     return out.value
 
@@ -574,7 +578,7 @@ class GASLoC:
             return
         self.stream.wait_stream(current)
         for t in tensors:
-            t.record_stream(self.stream)
+            t.record_stream(self.stream)  # their memory is not given out again before the call is done with it
         call(self.ctx, *args)
         current.wait_stream(self.stream)
 
@@ -669,21 +673,28 @@ class GASLoC:
                   rp, x, x_ld, stats, dout, d_ld, x.dtype, dx, ld, grads, gld, bool(accumulate), ws, size)
         return dx
 
-    def linear(self, weight, out_features, in_features, x, row_ptr, out=None):
+    def _linear_workspace(self, workspace, out_features, in_features, rp, dtype, device):
+        need = 0 if workspace is not None else gasloc_linear_workspace(self.ctx, out_features, in_features, rp, dtype)
+        return self._workspace(workspace, need, device)
+
+    def linear(self, weight, out_features, in_features, x, row_ptr, out=None, workspace=None):
         """out[t] = W_i x[t], W_i the [out_features, in_features] matrix at column `weight` of worker i's row."""
         rp, rows, device = self._layer(row_ptr)
         x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
         out, ld = self._out("out", out, rows, out_features, x.dtype, device)
-        self._run(gasloc_linear, (x, out), weight, out_features, in_features, rp, x, x_ld, x.dtype, out, ld)
+        ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
+        self._run(gasloc_linear, (x, out, ws), weight, out_features, in_features, rp, x, x_ld, x.dtype, out, ld, ws,
+                  size)
         return out
 
-    def linear_grad_input(self, weight, out_features, in_features, dout, row_ptr, dx=None):
+    def linear_grad_input(self, weight, out_features, in_features, dout, row_ptr, dx=None, workspace=None):
         """dx[t] = W_i^T dout[t]."""
         rp, rows, device = self._layer(row_ptr)
         d_ld = _rows_of("dout", dout, rows, out_features, dout.dtype, device)
         dx, ld = self._out("dx", dx, rows, in_features, dout.dtype, device)
-        self._run(gasloc_linear_grad_input, (dout, dx), weight, out_features, in_features, rp, dout, d_ld, dout.dtype,
-                  dx, ld)
+        ws, size = self._linear_workspace(workspace, out_features, in_features, rp, dout.dtype, device)
+        self._run(gasloc_linear_grad_input, (dout, dx, ws), weight, out_features, in_features, rp, dout, d_ld,
+                  dout.dtype, dx, ld, ws, size)
         return dx
 
     def linear_grad_weight(self, weight, out_features, in_features, x, dout, row_ptr, grads, accumulate=False,
@@ -693,8 +704,7 @@ class GASLoC:
         x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
         d_ld = _rows_of("dout", dout, rows, out_features, x.dtype, device)
         gld = self._grads(grads, device)
-        ws, size = self._workspace(
-            workspace, gasloc_linear_grad_weight_workspace(self.ctx, out_features, in_features, rp), device)
+        ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
         self._run(gasloc_linear_grad_weight, (x, dout, grads, ws), weight, out_features, in_features, rp, x, x_ld,
                   dout, d_ld, x.dtype, grads, gld, bool(accumulate), ws, size)
 

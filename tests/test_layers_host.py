@@ -18,12 +18,12 @@ def test_null_context():
     assert lib.gasloc_embedding_grad(None, 0, 1, 1, 1.0, ptr, None, 0, None, 1, None, 4, 0, None, 0) == BAD
     assert lib.gasloc_layer_norm(None, 0, 0, 1, 1e-5, ptr, None, 1, 0, None, 1, None) == BAD
     assert lib.gasloc_layer_norm_grad(None, 0, 0, 1, ptr, None, 1, None, None, 1, 0, None, 1, None, 4, 0, None, 0) == BAD
-    assert lib.gasloc_linear(None, 0, 1, 1, ptr, None, 1, 0, None, 1) == BAD
-    assert lib.gasloc_linear_grad_input(None, 0, 1, 1, ptr, None, 1, 0, None, 1) == BAD
+    assert lib.gasloc_linear(None, 0, 1, 1, ptr, None, 1, 0, None, 1, None, 0) == BAD
+    assert lib.gasloc_linear_grad_input(None, 0, 1, 1, ptr, None, 1, 0, None, 1, None, 0) == BAD
     assert lib.gasloc_linear_grad_weight(None, 0, 1, 1, ptr, None, 1, None, 1, 0, None, 4, 0, None, 0) == BAD
     assert lib.gasloc_embedding_grad_workspace(None, 1, ptr, ctypes.byref(size)) == BAD
     assert lib.gasloc_layer_norm_grad_workspace(None, 1, ptr, ctypes.byref(size)) == BAD
-    assert lib.gasloc_linear_grad_weight_workspace(None, 1, 1, ptr, ctypes.byref(size)) == BAD
+    assert lib.gasloc_linear_workspace(None, 1, 1, ptr, 0, ctypes.byref(size)) == BAD
     assert "NULL" in g.gasloc.gasloc_last_error(None)
 
 
