@@ -237,8 +237,8 @@ bool linear_tiles(int n, const int64_t* row_ptr, gasloc::LinearPass pass, int ti
 }
 
 // Splits the sums of a product whose tiles are fewer than two per CU, so that about two workgroups per CU share the
-// steps of k; a part has at least 16 steps (8 of fp32, which take longer), which cost about what writing and adding
-// a part does.  n = 3, 1111 rows, 513 x 257, fp32: 45 tiles 78 us, split 23 us.  Returns the bytes of the parts.
+// steps of k; a part of a full tile has at least 16 steps (8 of fp32, which take longer), which cost about what writing
+// and adding it does, one of a tile with fewer outputs accordingly fewer, down to 4.  n = 3, 1111 rows, 513 x 257, fp32: 45 tiles 78 us, split 23 us.  Returns the bytes of the parts.
 size_t split_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass pass, int32_t dtype,
                     gasloc::LinearArgs* a) {
   const int n = c.n;
@@ -255,7 +255,10 @@ size_t split_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearP
     steps[i] = (depth + per_step - 1) / per_step;
     work += tiles[i] * steps[i];
   }
-  int64_t part = std::max<int64_t>(dtype == GASLOC_BF16 ? 16 : 8, (work + want - 1) / want);
+  const int64_t wide = pass == gasloc::kLinearForward ? a->out_features : a->in_features;
+  const int64_t tall = pass == gasloc::kLinearWeight ? static_cast<int64_t>(n) * a->out_features : row_ptr[n];
+  const int64_t full = dtype == GASLOC_BF16 ? 16 : 8, outputs = tall * wide / total;  // per tile
+  int64_t part = std::max<int64_t>({4, full * outputs / (128 * 128), (work + want - 1) / want});
   part = (part + 3) / 4 * 4;
   bool any = false;
   for (int i = 0; i < n; ++i) any = any || (tiles[i] > 0 && steps[i] > part);
@@ -419,9 +422,9 @@ gasloc_status gasloc_embedding_grad(gasloc_ctx* c, int64_t begin, int32_t vocab,
     a.accumulate = accumulate;
     a.rows = row_spans(n, row_ptr);
     a.chunks = item_spans(n, row_ptr, a.chunk);
-    // Rows without tokens are zeroed about 16 KB to a workgroup, in the order of the rows: what is written at any
+    // Rows without tokens are zeroed about 16 KB to a workgroup (or four rows), in the order of the rows: what is written at any
     // time is one stretch of memory (1 MB each, n = 16 tables of 32000 x 1024: 454 us; 256 KB: 436; 16 KB: 358 us).
-    a.fill_rows = static_cast<int32_t>(std::min<int64_t>(gasloc::kMaxChunk, std::max<int64_t>(1, 4096 / width)));
+    a.fill_rows = static_cast<int32_t>(std::min<int64_t>(gasloc::kMaxChunk, std::max<int64_t>(4, 4096 / width)));
     HIP_TRY(c, gasloc::launch_embedding_sums(a, dtype, c->stream));
     if (rows > a.chunk) HIP_TRY(c, gasloc::launch_embedding_join(a, c->stream));
     return GASLOC_OK;
