@@ -345,8 +345,18 @@ def _row_ptr(a):
 # Layers over the workers' rows (include/gasloc_layers.h).  row_ptr: n + 1 host numbers; activations, tokens,
 # gradients and workspaces: torch device tensors (or addresses).
 
+_ACT = {}
+
+
 def _act(dtype):
     """gasloc_dtype of an activation given by name, code or torch dtype."""
+    code = _ACT.get(dtype)
+    if code is None:
+        code = _ACT[dtype] = _act_code(dtype)
+    return code
+
+
+def _act_code(dtype):
     if dtype in ("bf16", GASLOC_BF16) or str(dtype) == "torch.bfloat16":
         return GASLOC_BF16
     if dtype in ("f32", GASLOC_F32) or str(dtype) == "torch.float32":
@@ -567,20 +577,26 @@ class GASLoC:
             raise ValueError("row_ptr needs %d numbers" % (self.n + 1))
         return rp, int(rp[-1]), self.bufs["x"].device
 
-    def _run(self, call, tensors, *args):
-        """A call on the context's stream, in order with the current one: it sees what the current stream has
-        enqueued, and what that enqueues next sees the results."""
+    def _run(self, name, tensors, *args):
+        """The library's call `name` on the context's stream, in order with the current one: it sees what the
+        current stream has enqueued, and what that enqueues next sees the results."""
         import torch
 
-        current = torch.cuda.current_stream(self.stream.device)
-        if current.cuda_stream == self.stream.cuda_stream:
-            call(self.ctx, *args)
-            return
-        self.stream.wait_stream(current)
-        for t in tensors:
-            t.record_stream(self.stream)  # their memory is not given out again before the call is done with it
-        call(self.ctx, *args)
-        current.wait_stream(self.stream)
+        fn = getattr(library(), name)
+        # the current stream's handle alone where torch gives it, a tenth of the time that the stream takes
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        device = self.stream.device_index
+        if (raw(device) if raw else torch.cuda.current_stream(device).cuda_stream) == self.stream.cuda_stream:
+            status = fn(self.ctx, *args)
+        else:
+            current = torch.cuda.current_stream(device)
+            self.stream.wait_stream(current)
+            for t in tensors:
+                t.record_stream(self.stream)  # their memory is not given out again before the call is done with it
+            status = fn(self.ctx, *args)
+            current.wait_stream(self.stream)
+        if status != GASLOC_OK:
+            _check(status, self.ctx)
 
     def _out(self, name, t, rows, cols, dtype, device):
         """The tensor a result goes to (a new one for None) and its row length."""
@@ -631,7 +647,8 @@ class GASLoC:
         code = _act(out.dtype if out is not None else self.bufs["x"].dtype if dtype is None else dtype)
         out, ld = self._out("out", out, rows, width, torch.bfloat16 if code == GASLOC_BF16 else torch.float32, device)
         self._tokens(tokens, rows, device)
-        self._run(gasloc_embedding, (tokens, out), table, vocab, width, scale, rp, tokens, code, out, ld)
+        self._run("gasloc_embedding", (tokens, out), int(table), int(vocab), int(width), float(scale),
+                  rp.ctypes.data, tokens.data_ptr(), code, out.data_ptr(), ld)
         return out
 
     def embedding_grad(self, table, vocab, width, tokens, row_ptr, dout, grads, scale=1.0, accumulate=False,
@@ -642,8 +659,9 @@ class GASLoC:
         gld = self._grads(grads, device)
         self._tokens(tokens, rows, device)
         ws, size = self._workspace(workspace, gasloc_embedding_grad_workspace(self.ctx, width, rp), device)
-        self._run(gasloc_embedding_grad, (tokens, dout, grads, ws), table, vocab, width, scale, rp, tokens, dout.dtype,
-                  dout, ld, grads, gld, bool(accumulate), ws, size)
+        self._run("gasloc_embedding_grad", (tokens, dout, grads, ws), int(table), int(vocab), int(width), float(scale),
+                  rp.ctypes.data, tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld, grads.data_ptr(), gld,
+                  bool(accumulate), ws.data_ptr(), size)
 
     def layer_norm(self, gain, bias, width, x, row_ptr, eps=1e-5, out=None, stats=None):
         """(out, stats): the normalised rows (gain and bias at these columns; bias None: none) and every
@@ -652,8 +670,8 @@ class GASLoC:
         x_ld = _rows_of("x", x, rows, width, x.dtype, device)
         out, ld = self._out("out", out, rows, width, x.dtype, device)
         stats = self._stats(stats, rows, device)
-        self._run(gasloc_layer_norm, (x, out, stats), gain, -1 if bias is None else bias, width, eps, rp, x, x_ld,
-                  x.dtype, out, ld, stats)
+        self._run("gasloc_layer_norm", (x, out, stats), int(gain), -1 if bias is None else int(bias), int(width),
+                  float(eps), rp.ctypes.data, x.data_ptr(), x_ld, _act(x.dtype), out.data_ptr(), ld, stats.data_ptr())
         return out, stats
 
     def layer_norm_grad(self, gain, bias, width, x, row_ptr, stats, dout, grads, dx=None, accumulate=False,
@@ -669,8 +687,10 @@ class GASLoC:
         stats = self._stats(stats, rows, device)
         gld = self._grads(grads, device)
         ws, size = self._workspace(workspace, gasloc_layer_norm_grad_workspace(self.ctx, width, rp), device)
-        self._run(gasloc_layer_norm_grad, (x, stats, dout, dx, grads, ws), gain, -1 if bias is None else bias, width,
-                  rp, x, x_ld, stats, dout, d_ld, x.dtype, dx, ld, grads, gld, bool(accumulate), ws, size)
+        self._run("gasloc_layer_norm_grad", (x, stats, dout, dx, grads, ws), int(gain),
+                  -1 if bias is None else int(bias), int(width), rp.ctypes.data, x.data_ptr(), x_ld, stats.data_ptr(),
+                  dout.data_ptr(), d_ld, _act(x.dtype), dx.data_ptr(), ld, grads.data_ptr(), gld, bool(accumulate),
+                  ws.data_ptr(), size)
         return dx
 
     def _linear_workspace(self, workspace, out_features, in_features, rp, dtype, device):
@@ -683,8 +703,8 @@ class GASLoC:
         x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
         out, ld = self._out("out", out, rows, out_features, x.dtype, device)
         ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
-        self._run(gasloc_linear, (x, out, ws), weight, out_features, in_features, rp, x, x_ld, x.dtype, out, ld, ws,
-                  size)
+        self._run("gasloc_linear", (x, out, ws), int(weight), int(out_features), int(in_features),
+                  rp.ctypes.data, x.data_ptr(), x_ld, _act(x.dtype), out.data_ptr(), ld, ws.data_ptr(), size)
         return out
 
     def linear_grad_input(self, weight, out_features, in_features, dout, row_ptr, dx=None, workspace=None):
@@ -693,8 +713,8 @@ class GASLoC:
         d_ld = _rows_of("dout", dout, rows, out_features, dout.dtype, device)
         dx, ld = self._out("dx", dx, rows, in_features, dout.dtype, device)
         ws, size = self._linear_workspace(workspace, out_features, in_features, rp, dout.dtype, device)
-        self._run(gasloc_linear_grad_input, (dout, dx, ws), weight, out_features, in_features, rp, dout, d_ld,
-                  dout.dtype, dx, ld, ws, size)
+        self._run("gasloc_linear_grad_input", (dout, dx, ws), int(weight), int(out_features), int(in_features),
+                  rp.ctypes.data, dout.data_ptr(), d_ld, _act(dout.dtype), dx.data_ptr(), ld, ws.data_ptr(), size)
         return dx
 
     def linear_grad_weight(self, weight, out_features, in_features, x, dout, row_ptr, grads, accumulate=False,
@@ -705,8 +725,9 @@ class GASLoC:
         d_ld = _rows_of("dout", dout, rows, out_features, x.dtype, device)
         gld = self._grads(grads, device)
         ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
-        self._run(gasloc_linear_grad_weight, (x, dout, grads, ws), weight, out_features, in_features, rp, x, x_ld,
-                  dout, d_ld, x.dtype, grads, gld, bool(accumulate), ws, size)
+        self._run("gasloc_linear_grad_weight", (x, dout, grads, ws), int(weight), int(out_features), int(in_features),
+                  rp.ctypes.data, x.data_ptr(), x_ld, dout.data_ptr(), d_ld, _act(x.dtype), grads.data_ptr(), gld,
+                  bool(accumulate), ws.data_ptr(), size)
 
     def counters(self):
         """(k, stepped, rounds_done): per-worker AdamW step counts, which workers
