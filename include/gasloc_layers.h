@@ -8,7 +8,7 @@
  * Conventions, beside those of gasloc.h:
  *   - Token rows.  A call takes the token rows of all workers, packed: worker
  *     i has rows row_ptr[i] .. row_ptr[i+1] - 1 of every activation.  row_ptr:
- *     host int64[n+1], row_ptr[0] = 0, non-decreasing, row_ptr[n] <= 2^30.  A
+ *     host int64[n+1], row_ptr[0] = 0, non-decreasing, row_ptr[n] <= 2^27.  A
  *     worker may have none.  Rows from row_ptr[n] on are neither read nor
  *     written.  The counts go with the launch: a call recorded in a HIP graph
  *     keeps them.
@@ -85,7 +85,7 @@ gasloc_status gasloc_embedding_grad_workspace(const gasloc_ctx *ctx, int32_t wid
  *   out[t, c] = (x[t, c] - mean) * rstd * gain_i[c] + bias_i[c].
  * gain, bias: the columns at which the two vectors start; bias < 0: none.
  * width in [1, 16384]; eps finite and > 0.  x and out have the same dtype;
- * out may be x.  stats: device fp32 [row_ptr[n], 2], 8-byte aligned, receives
+ * out may be x (with the same row length).  stats: device fp32 [row_ptr[n], 2], 8-byte aligned, receives
  * (mean, rstd) of every row for the backward pass; NULL: not kept.  Enqueues
  * one kernel. */
 gasloc_status gasloc_layer_norm(gasloc_ctx *ctx, int64_t gain, int64_t bias, int32_t width, float eps,
@@ -97,7 +97,7 @@ gasloc_status gasloc_layer_norm(gasloc_ctx *ctx, int64_t gain, int64_t bias, int
  *   dx[t, :] = rstd * (h - mean_c(h) - xh * mean_c(h * xh))
  *   grads_i[gain + c] (+)= sum_t dout[t, c] * xh[t, c]
  *   grads_i[bias + c] (+)= sum_t dout[t, c]              (bias >= 0)
- * stats: what the forward pass kept.  dx may be dout or x.  Enqueues two
+ * stats: what the forward pass kept.  dx may be dout or x (with the same row length).  Enqueues two
  * kernels.  workspace: at least gasloc_layer_norm_grad_workspace bytes. */
 gasloc_status gasloc_layer_norm_grad(gasloc_ctx *ctx, int64_t gain, int64_t bias, int32_t width,
                                      const int64_t *row_ptr, const void *x, int64_t x_ld, const float *stats,

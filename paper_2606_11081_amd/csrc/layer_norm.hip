@@ -7,6 +7,10 @@
 // pass's two means are taken.  One wave per row up to 2048 columns, then a
 // workgroup of 4 or 8 waves; a workgroup takes tile_rows rows of one worker
 // with that worker's gain and bias in registers.
+//
+// Measured (n = 16, 65536 rows of 1024, bf16 rows, fp32 weights): forward 52 us
+// (269 MB, 5.2 TB/s), backward 87 us (403 MB, 4.6 TB/s), 5 of them the join of
+// the partial sums; n = 7, 5003 rows of 1023, fp32: backward 22 us (2.8 TB/s).
 #pragma clang fp contract(off)
 
 #include <type_traits>
@@ -72,7 +76,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm(
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       float v[V] = {};
-      if (c0 + j * kStep < a.width) load_row<AT, V, true>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, left(j), v);
+      if (c0 + j * kStep < a.width)
+        load_row<AT, V, true>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, left(j), v);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         x[j * V + e] = v[e];
@@ -283,17 +288,21 @@ int norm_waves(int width) { return norm_shape(width).waves; }
 
 hipError_t launch_layer_norm(const NormArgs& a, int params, int act, bool whole, hipStream_t stream) {
   if (params == GASLOC_BF16)
-    return whole ? forward<GASLOC_BF16, GASLOC_BF16, true>(a, stream) : forward<GASLOC_BF16, GASLOC_BF16, false>(a, stream);
+    return whole ? forward<GASLOC_BF16, GASLOC_BF16, true>(a, stream)
+                 : forward<GASLOC_BF16, GASLOC_BF16, false>(a, stream);
   if (act == GASLOC_BF16)
-    return whole ? forward<GASLOC_F32, GASLOC_BF16, true>(a, stream) : forward<GASLOC_F32, GASLOC_BF16, false>(a, stream);
+    return whole ? forward<GASLOC_F32, GASLOC_BF16, true>(a, stream)
+                 : forward<GASLOC_F32, GASLOC_BF16, false>(a, stream);
   return whole ? forward<GASLOC_F32, GASLOC_F32, true>(a, stream) : forward<GASLOC_F32, GASLOC_F32, false>(a, stream);
 }
 
 hipError_t launch_layer_norm_grad(const NormGradArgs& a, int params, int act, bool whole, hipStream_t stream) {
   if (params == GASLOC_BF16)
-    return whole ? backward<GASLOC_BF16, GASLOC_BF16, true>(a, stream) : backward<GASLOC_BF16, GASLOC_BF16, false>(a, stream);
+    return whole ? backward<GASLOC_BF16, GASLOC_BF16, true>(a, stream)
+                 : backward<GASLOC_BF16, GASLOC_BF16, false>(a, stream);
   if (act == GASLOC_BF16)
-    return whole ? backward<GASLOC_F32, GASLOC_BF16, true>(a, stream) : backward<GASLOC_F32, GASLOC_BF16, false>(a, stream);
+    return whole ? backward<GASLOC_F32, GASLOC_BF16, true>(a, stream)
+                 : backward<GASLOC_F32, GASLOC_BF16, false>(a, stream);
   return whole ? backward<GASLOC_F32, GASLOC_F32, true>(a, stream) : backward<GASLOC_F32, GASLOC_F32, false>(a, stream);
 }
 

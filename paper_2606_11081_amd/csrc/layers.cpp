@@ -3,7 +3,6 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
-#include <climits>
 #include <cmath>
 #include <string>
 
@@ -23,7 +22,9 @@ using gasloc::Spans;
 
 namespace {
 
-constexpr int64_t kMaxRows = int64_t(1) << 30;
+// A launch holds fewer than 2^32 threads; at most 16 of them go with a row.
+constexpr int64_t kMaxRows = int64_t(1) << 27;
+constexpr int64_t kMaxGroups = 0xffffffffll / 512;  // of a linear layer's launch
 constexpr int64_t kMaxLd = int64_t(1) << 21;
 
 // Nothing but a status leaves the library: building a message may run out of memory.
@@ -47,7 +48,7 @@ std::string check_rows(int n, const int64_t* row_ptr) {
   if (row_ptr[0] != 0) return "row_ptr must start at 0";
   for (int i = 0; i < n; ++i)
     if (row_ptr[i + 1] < row_ptr[i]) return format("row_ptr decreases at worker %d", i);
-  if (row_ptr[n] > kMaxRows) return "more than 2^30 rows";
+  if (row_ptr[n] > kMaxRows) return "more than 2^27 rows";
   return "";
 }
 
@@ -67,9 +68,15 @@ std::string check_columns(const gasloc_ctx& c, const char* what, int64_t begin, 
 // An activation of `rows` rows of `cols` elements.
 std::string check_act(const char* what, const void* p, int64_t ld, int64_t cols, int64_t rows, int32_t dtype) {
   if (rows > 0 && !p) return format("%s must not be NULL", what);
-  if (reinterpret_cast<uintptr_t>(p) % param_bytes(dtype) != 0) return format("%s is not aligned to its elements", what);
+  if (reinterpret_cast<uintptr_t>(p) % param_bytes(dtype) != 0)
+    return format("%s is not aligned to its elements", what);
   if (ld < cols || ld >= kMaxLd) return format("%s: row length must be in [%lld, 2^21)", what, (long long)cols);
   return "";
+}
+
+// A result may take the place of an operand if their rows are the same.
+std::string check_in_place(const char* what, const void* a, int64_t a_ld, const void* b, int64_t b_ld) {
+  return a && a == b && a_ld != b_ld ? format("%s: rows of another length in the same place", what) : std::string();
 }
 
 std::string check_grads(const gasloc_ctx& c, const float* grads, int64_t grad_ld, int32_t accumulate) {
@@ -121,7 +128,9 @@ bool vector_rows(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
 }
 
 // The same for a weight at column `begin` of the parameters and of the gradients.
-bool vector_columns(const gasloc_ctx& c, int64_t begin) { return begin * static_cast<int64_t>(param_bytes(c.hp.param_dtype)) % 16 == 0; }
+bool vector_columns(const gasloc_ctx& c, int64_t begin) {
+  return begin * static_cast<int64_t>(param_bytes(c.hp.param_dtype)) % 16 == 0;
+}
 
 size_t round256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -229,7 +238,7 @@ bool linear_tiles(int n, const int64_t* row_ptr, gasloc::LinearPass pass, int ti
     at += pass == gasloc::kLinearWeight    ? cut(a->out_features) * cut(a->in_features)
           : pass == gasloc::kLinearForward ? cut(rows) * cut(a->out_features)
                                            : cut(rows) * cut(a->in_features);
-    if (at > INT_MAX) return false;
+    if (at > kMaxGroups) return false;
     a->tiles.begin[i + 1] = static_cast<int32_t>(at);
     a->parts.begin[i + 1] = i + 1;
   }
@@ -237,8 +246,9 @@ bool linear_tiles(int n, const int64_t* row_ptr, gasloc::LinearPass pass, int ti
 }
 
 // Splits the sums of a product whose tiles are fewer than two per CU, so that about two workgroups per CU share the
-// steps of k; a part of a full tile has at least 16 steps (8 of fp32, which take longer), which cost about what writing
-// and adding it does, one of a tile with fewer outputs accordingly fewer, down to 4.  n = 3, 1111 rows, 513 x 257, fp32: 45 tiles 78 us, split 23 us.  Returns the bytes of the parts.
+// steps of k; a part of a full tile has at least 16 steps, which cost about what writing and adding it does, one of
+// a tile with fewer outputs accordingly fewer, down to 4.  n = 3, 1111 rows, 513 x 257, fp32: 45 tiles 78 us, split
+// 23 us.  Returns the bytes of the parts.
 size_t split_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass pass, int32_t dtype,
                     gasloc::LinearArgs* a) {
   const int n = c.n;
@@ -257,8 +267,8 @@ size_t split_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearP
   }
   const int64_t wide = pass == gasloc::kLinearForward ? a->out_features : a->in_features;
   const int64_t tall = pass == gasloc::kLinearWeight ? static_cast<int64_t>(n) * a->out_features : row_ptr[n];
-  const int64_t full = dtype == GASLOC_BF16 ? 16 : 8, outputs = tall * wide / total;  // per tile
-  int64_t part = std::max<int64_t>({4, full * outputs / (128 * 128), (work + want - 1) / want});
+  const int64_t outputs = tall * wide / total;  // per tile
+  int64_t part = std::max<int64_t>({4, 16 * outputs / (128 * 128), (work + want - 1) / want});
   part = (part + 3) / 4 * 4;
   bool any = false;
   for (int i = 0; i < n; ++i) any = any || (tiles[i] > 0 && steps[i] > part);
@@ -290,8 +300,8 @@ gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPas
   int64_t most = 0;
   for (int i = 0; i < c->n; ++i) most = std::max(most, row_ptr[i + 1] - row_ptr[i]);
   int tile = vec && dtype == GASLOC_BF16 ? 256 : 128;
-  // Few rows: the weights' way through LDS in tiles of 128 outputs leaves too few loads in flight (n = 16, one row each,
-  // 2048 -> 2048, bf16 rows, fp32 weights: 61 us against 48, bf16 weights 28).
+  // Few rows: the weights' way through LDS in tiles of 128 outputs leaves too few loads in flight (n = 16, one row
+  // each, 2048 -> 2048, bf16 rows, fp32 weights: 61 us against 48).
   if (pass == gasloc::kLinearForward && most <= gasloc::kFewRows) tile = gasloc::kFewRows;
   bool fits = linear_tiles(c->n, row_ptr, pass, tile, a);
   if (fits && tile == 256 && a->tiles.begin[c->n] < 2 * c->cus) {
@@ -422,8 +432,9 @@ gasloc_status gasloc_embedding_grad(gasloc_ctx* c, int64_t begin, int32_t vocab,
     a.accumulate = accumulate;
     a.rows = row_spans(n, row_ptr);
     a.chunks = item_spans(n, row_ptr, a.chunk);
-    // Rows without tokens are zeroed about 16 KB to a workgroup (or four rows), in the order of the rows: what is written at any
-    // time is one stretch of memory (1 MB each, n = 16 tables of 32000 x 1024: 454 us; 256 KB: 436; 16 KB: 358 us).
+    // Rows without tokens are zeroed about 16 KB to a workgroup (or four rows), in the order of the rows: what is
+    // written at any time is one stretch of memory (n = 16 tables of 32000 x 1024, 1 MB each: 454 us; 256 KB: 436;
+    // 16 KB: 358).
     a.fill_rows = static_cast<int32_t>(std::min<int64_t>(gasloc::kMaxChunk, std::max<int64_t>(4, 4096 / width)));
     HIP_TRY(c, gasloc::launch_embedding_sums(a, dtype, c->stream));
     if (rows > a.chunk) HIP_TRY(c, gasloc::launch_embedding_join(a, c->stream));
@@ -444,6 +455,7 @@ gasloc_status gasloc_layer_norm(gasloc_ctx* c, int64_t gain, int64_t bias, int32
     const int64_t rows = row_ptr[c->n];
     CHECK(c, check_act("x", x, x_ld, width, rows, dtype));
     CHECK(c, check_act("out", out, out_ld, width, rows, dtype));
+    CHECK(c, check_in_place("out", out, out_ld, x, x_ld));
     if (reinterpret_cast<uintptr_t>(stats) % 8 != 0) return fail(c, GASLOC_EINVAL, "stats must be 8-byte aligned");
     if (rows == 0) return GASLOC_OK;
     gasloc::NormArgs a{};
@@ -495,6 +507,8 @@ gasloc_status gasloc_layer_norm_grad(gasloc_ctx* c, int64_t gain, int64_t bias, 
     CHECK(c, check_act("x", x, x_ld, width, rows, dtype));
     CHECK(c, check_act("dout", dout, dout_ld, width, rows, dtype));
     CHECK(c, check_act("dx", dx, dx_ld, width, rows, dtype));
+    CHECK(c, check_in_place("dx", dx, dx_ld, dout, dout_ld));
+    CHECK(c, check_in_place("dx", dx, dx_ld, x, x_ld));
     if ((rows > 0 && !stats) || reinterpret_cast<uintptr_t>(stats) % 8 != 0)
       return fail(c, GASLOC_EINVAL, "stats must be non-NULL and 8-byte aligned");
     CHECK(c, check_grads(*c, grads, grad_ld, accumulate));
@@ -590,7 +604,8 @@ gasloc_status gasloc_linear_workspace(const gasloc_ctx* c, int32_t out_features,
       gasloc::LinearArgs a{};
       a.out_features = out_features;
       a.in_features = in_features;
-      if (linear_tiles(c->n, row_ptr, pass, 128, &a)) *bytes = std::max(*bytes, split_linear(*c, row_ptr, pass, dtype, &a));
+      if (linear_tiles(c->n, row_ptr, pass, 128, &a))
+        *bytes = std::max(*bytes, split_linear(*c, row_ptr, pass, dtype, &a));
     }
     *bytes = round256(*bytes);
     return GASLOC_OK;

@@ -159,8 +159,9 @@ struct LinearArgs {
 constexpr int kLinearStep = 64;  // bytes of k per step; the kernel takes four at a time
 constexpr int kFewRows = 16;
 // tile: rows and columns of a workgroup's part of C (256, or 128: always 128 without vec and in F32; kFewRows:
-// forward pass of workers with at most so many rows, 16 outputs of all of them per workgroup); vec: every row of either operand, of C and of
-// the gradients begins on a 16-byte boundary and is a whole number of 16-byte chunks of activations.
+// forward pass of workers with at most so many rows, 16 outputs of all of them per workgroup).  vec: every row of
+// either operand, of C and of the gradients begins on a 16-byte boundary and is a whole number of 16-byte chunks
+// of activations.
 hipError_t launch_linear(const LinearArgs& a, LinearPass pass, int params, int act, int tile, bool vec,
                          hipStream_t stream);
 

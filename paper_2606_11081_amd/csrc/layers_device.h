@@ -147,7 +147,8 @@ __device__ __forceinline__ void store_row(void* base, int64_t idx, int left, con
 // lanes, then the four row sums in order.
 __device__ __forceinline__ float wave_sum_f32(float v) {
   const auto shifted = [](float x, auto k) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x110 + decltype(k)::value, 0xf, 0xf, true));
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x110 + decltype(k)::value, 0xf, 0xf, true));
   };
   v += shifted(v, std::integral_constant<int, 1>{});
   v += shifted(v, std::integral_constant<int, 2>{});

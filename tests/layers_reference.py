@@ -63,7 +63,8 @@ def layer_norm(x, gain, bias, row_ptr, eps, act):
     e_mean = 68 * U * np.abs(x).mean(1)
     e_var = 2 * e_mean * np.abs(d).mean(1) + e_mean ** 2 + 72 * U * var
     e_rstd = e_var / (2 * (var + eps)) + 4 * U  # relative
-    e = np.abs(gain[worker]) * (rstd[:, None] * (e_mean[:, None] + U * np.abs(d)) + np.abs(hat) * (e_rstd[:, None] + 4 * U))
+    e = rstd[:, None] * (e_mean[:, None] + U * np.abs(d)) + np.abs(hat) * (e_rstd[:, None] + 4 * U)
+    e = np.abs(gain[worker]) * e
     e = 1.01 * e + 2 * U * np.abs(out)
     e += (HALF_STEP[act] if act == "bf16" else 0) * (np.abs(out) + e) + TINY
     e_stats = np.stack((1.01 * e_mean, 1.01 * e_rstd * rstd), 1) + TINY

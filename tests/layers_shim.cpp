@@ -33,10 +33,16 @@ static int g_tile = 0, g_vec = 0, g_merges = 0;
 hipError_t launch_embedding(const EmbeddingArgs&, int, int, hipStream_t) { return ++g_launches, hipSuccess; }
 hipError_t launch_token_sort(const SortArgs&, hipStream_t) { return ++g_launches, hipSuccess; }
 hipError_t launch_token_merge(const MergeArgs&, hipStream_t) { return ++g_merges, ++g_launches, hipSuccess; }
-hipError_t launch_embedding_sums(const EmbeddingGradArgs& a, int, hipStream_t) { return g_sums = a, ++g_launches, hipSuccess; }
+hipError_t launch_embedding_sums(const EmbeddingGradArgs& a, int, hipStream_t) {
+  g_sums = a;
+  return ++g_launches, hipSuccess;
+}
 hipError_t launch_embedding_join(const EmbeddingGradArgs&, hipStream_t) { return ++g_launches, hipSuccess; }
 hipError_t launch_layer_norm(const NormArgs&, int, int, bool, hipStream_t) { return ++g_launches, hipSuccess; }
-hipError_t launch_layer_norm_grad(const NormGradArgs& a, int, int, bool, hipStream_t) { return g_norm = a, ++g_launches, hipSuccess; }
+hipError_t launch_layer_norm_grad(const NormGradArgs& a, int, int, bool, hipStream_t) {
+  g_norm = a;
+  return ++g_launches, hipSuccess;
+}
 hipError_t launch_layer_norm_join(const NormGradArgs&, hipStream_t) { return ++g_launches, hipSuccess; }
 int norm_waves(int width) { return width <= 2048 ? 1 : width <= 8192 ? 4 : 8; }
 hipError_t launch_linear(const LinearArgs& a, LinearPass, int, int, int tile, bool vec, hipStream_t) {

@@ -121,7 +121,7 @@ REFUSALS = [
     ("gasloc_*", dict(row_ptr=None), "row_ptr must not be NULL"),
     ("gasloc_*", dict(ptr=np.array([1, 2, 3, 4, 5], np.int64)), "start at 0"),
     ("gasloc_*", dict(ptr=np.array([0, 4, 3, 4, 5], np.int64)), "decreases at worker 1"),
-    ("gasloc_*", dict(ptr=rp(1 << 30, 0, 1, 0)), "more than 2^30 rows"),
+    ("gasloc_*", dict(ptr=rp(1 << 27, 0, 1, 0)), "more than 2^27 rows"),
     ("gasloc_*", dict(dtype=2), "dtype must be"),
     ("gasloc_*", dict(dtype=-1), "dtype must be"),
     ("gasloc_embedding*", dict(begin=-1), "table: columns"),
@@ -145,6 +145,9 @@ REFUSALS = [
     ("gasloc_layer_norm", dict(eps=float("nan")), "eps must be"),
     ("gasloc_layer_norm*", dict(stats=P0 + 4), "stats must be"),
     ("gasloc_layer_norm_grad", dict(stats=None), "stats must be"),
+    ("gasloc_layer_norm", dict(out_ld=72), "rows of another length"),
+    ("gasloc_layer_norm_grad", dict(dx_ld=72, dout=P0 + 0x1000), "rows of another length"),
+    ("gasloc_layer_norm_grad", dict(dx_ld=72, x=P0 + 0x1000), "rows of another length"),
     ("gasloc_linear*", dict(weight=-1), "weight: columns"),
     ("gasloc_linear*", dict(weight=100_000 - 2047), "weight: columns"),
     ("gasloc_linear*", dict(out_features=0), "features must be"),
@@ -214,9 +217,9 @@ def test_workspace_refusals(shim):
                  (ctx.c, 8, None, ctypes.byref(size)), (ctx.c, 8, ptr.ctypes.data, None)):
         assert shim.gasloc_embedding_grad_workspace(*args) == BAD
         assert shim.gasloc_layer_norm_grad_workspace(*args) == BAD
-    for args in ((None, 8, 8, ptr.ctypes.data, 0, ctypes.byref(size)), (ctx.c, 0, 8, ptr.ctypes.data, 0, ctypes.byref(size)),
-                 (ctx.c, 8, 1 << 21, ptr.ctypes.data, 0, ctypes.byref(size)), (ctx.c, 8, 8, None, 0, ctypes.byref(size)),
-                 (ctx.c, 8, 8, ptr.ctypes.data, 5, ctypes.byref(size)), (ctx.c, 8, 8, ptr.ctypes.data, 0, None)):
+    at, out = ptr.ctypes.data, ctypes.byref(size)
+    for args in ((None, 8, 8, at, 0, out), (ctx.c, 0, 8, at, 0, out), (ctx.c, 8, 1 << 21, at, 0, out),
+                 (ctx.c, 8, 8, None, 0, out), (ctx.c, 8, 8, at, 5, out), (ctx.c, 8, 8, at, 0, None)):
         assert shim.gasloc_linear_workspace(*args) == BAD
 
 
@@ -325,6 +328,16 @@ def test_norm_and_embedding_workspaces_hold_their_partial_sums(shim, seed):
     assert np.array_equal(np.diff(plan[2:]), -(-rows // plan[0]))
     sorts = 2 if rows.max() > 8192 else 1
     assert 8 * int(ptr[-1]) * sorts + 2 * 4 * int(plan[-1]) * width <= size.value
+
+
+def test_header_is_plain_c(tmp_path):
+    cc = shutil.which("gcc")
+    if not cc:
+        pytest.skip("no gcc")
+    src = tmp_path / "use.c"
+    src.write_text('#include "gasloc_layers.h"\nint main(void) { return gasloc_linear == 0; }\n')
+    subprocess.run([cc, "-std=c99", "-Wall", "-Wextra", "-Werror", "-pedantic", "-I" + os.path.join(ROOT, "include"),
+                    "-fsyntax-only", "-Wno-address", str(src)], check=True, capture_output=True)
 
 
 # --------------------------------------------------------------------------
