@@ -32,7 +32,8 @@
  *     an order that depends on the sizes alone: the same call gives the same
  *     bits again.
  *   - All work is enqueued on the context's stream; no call waits, allocates or
- *     copies, so each may be recorded in a graph.  Workspaces are the caller's
+ *     copies, so each may be recorded in a graph (of a context whose stream is not
+ *     the default one).  Workspaces are the caller's
  *     (device, 256-byte aligned; calls that may overlap in time, or graphs whose
  *     replays may, need one each); what one holds before or after a call does
  *     not matter.

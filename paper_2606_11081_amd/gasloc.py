@@ -590,6 +590,13 @@ class GASLoC:
             status = fn(self.ctx, *args)
         else:
             current = torch.cuda.current_stream(device)
+            # The default stream cannot be part of a graph, and waiting there for work that is only recorded ends
+            # the process.
+            if 0 in (self.stream.cuda_stream, current.cuda_stream):
+                with torch.cuda.stream(current if self.stream.cuda_stream == 0 else self.stream):
+                    if torch.cuda.is_current_stream_capturing():
+                        raise ValueError("a graph cannot hold calls of a context on the default stream, nor calls "
+                                         "from there: give the context the stream that is captured")
             self.stream.wait_stream(current)
             for t in tensors:
                 t.record_stream(self.stream)  # their memory is not given out again before the call is done with it

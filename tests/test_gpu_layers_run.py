@@ -169,6 +169,60 @@ def test_recorded_steps_replay(params, act):
         run.close()
 
 
+def test_graph_recorded_on_another_stream():
+    """A context with a stream of its own: calls recorded from another stream replay with the eager results."""
+    import torch
+
+    n, rows, width = 3, 300, 64
+    ptr = np.array([0, 100, 100, rows])
+    run = g.GASLoC(n, width * width, outer_momentum=0.0, consensus_momentum=0.0, stream=torch.cuda.Stream())
+    run.set_params(torch.empty(width * width, device="cuda").normal_(0.0, 0.05))
+    x = torch.empty((rows, width), device="cuda").normal_()
+    grads = torch.zeros((n, run.ld), device="cuda")
+
+    def step(into):
+        out = run.linear(0, width, width, x, ptr)
+        run.linear_grad_weight(0, width, width, x, out, ptr, into)
+        return out
+
+    step(grads)  # warm-up
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = step(grads)
+    for replay in range(4):
+        x.normal_()
+        other = torch.full_like(grads, 3.0)
+        eager = step(other)
+        grads.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(recorded, eager) and torch.equal(grads, other), replay
+    run.close()
+
+
+def test_graph_refuses_the_default_stream():
+    """A context on the default stream cannot take part in a graph: an error, and both go on."""
+    import torch
+
+    width, ptr = 64, np.array([0, 8, 16])
+    run = g.GASLoC(2, width * width, outer_momentum=0.0, consensus_momentum=0.0)
+    run.set_params(torch.empty(width * width, device="cuda").normal_(0.0, 0.05))
+    x = torch.empty((16, width), device="cuda").normal_()
+    out = torch.zeros_like(x)
+    expect = run.linear(0, width, width, x, ptr)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError, match="default stream"):
+            run.linear(0, width, width, x, ptr, out=out)
+        out.add_(1.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, torch.ones_like(out))
+    assert torch.equal(run.linear(0, width, width, x, ptr), expect)
+    run.close()
+
+
 def test_called_from_another_stream():
     """The context has a stream of its own; the program computes inputs and uses results on the current one, and
     frees them at once.  Nothing waits on the host."""
