@@ -245,47 +245,69 @@ bool linear_tiles(int n, const int64_t* row_ptr, gasloc::LinearPass pass, int ti
   return true;
 }
 
+// The length of a worker's sums.
+int64_t depth_of(const gasloc::LinearArgs& a, const int64_t* row_ptr, gasloc::LinearPass pass, int worker) {
+  return pass == gasloc::kLinearForward ? a.in_features
+         : pass == gasloc::kLinearInput ? a.out_features
+                                        : row_ptr[worker + 1] - row_ptr[worker];
+}
+
+// All outputs of the product.
+int64_t outputs_of(int n, const gasloc::LinearArgs& a, const int64_t* row_ptr, gasloc::LinearPass pass) {
+  return pass == gasloc::kLinearWeight ? static_cast<int64_t>(n) * a.out_features * a.in_features
+                                       : row_ptr[n] * (pass == gasloc::kLinearForward ? a.out_features : a.in_features);
+}
+
+// Cuts a product that tiles of 256 do not suit into tiles of 128 outputs, or of 64 where those would be too few for
+// the CUs (fewer than one per CU, or two in F32, whose matrix instructions take longer) and none would have many steps
+// to do (20 per CU in BF16, 128 in F32): such products wait for their loads, not for the matrix cores.  Others keep the
+// tiles of 128, which read half as much for an output.  Tiles of 128 / of 64, bf16: n = 4, 256 rows each, 512 -> 512
+// 7.9 / 5.4 us; n = 16, 512 rows, 512 -> 512 9.2 / 11.7; the weight's gradient of n = 4, 4096 rows, 512 -> 512 25 / 29;
+// fp32: n = 4, 600 rows, 1024 -> 2560 212 / 119.  Returns the side, 0 if the product is too large.
+int cut_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass pass, int32_t dtype,
+               gasloc::LinearArgs* a) {
+  if (!linear_tiles(c.n, row_ptr, pass, 128, a)) return 0;
+  const bool f32 = dtype == GASLOC_F32;
+  const int64_t full = static_cast<int64_t>(c.cus) * (128 * 128);  // outputs of one tile per CU
+  const int64_t products = row_ptr[c.n] * a->in_features;          // times out_features
+  if (outputs_of(c.n, *a, row_ptr, pass) >= (f32 ? 2 : 1) * full ||
+      products >= (f32 ? 128 * 16 : 20 * 32) * full / a->out_features)
+    return 128;
+  linear_tiles(c.n, row_ptr, pass, 64, a);
+  return 64;
+}
+
 // Splits the sums of a product whose tiles are fewer than two per CU, so that about two workgroups per CU share the
-// steps of k; a part of a full tile has at least 16 steps, which cost about what writing and adding it does, one of
-// a tile with fewer outputs accordingly fewer, down to 4.  n = 3, 1111 rows, 513 x 257, fp32: 45 tiles 78 us, split
-// 23 us.  Returns the bytes of the parts.
+// steps of k, if that saves more steps than the parts cost: the join's launch takes about as long as 16 steps (4 us),
+// and writing and adding a megabyte of parts as 2.  bf16, whole / split: n = 2, 64 rows each, 8192 -> 512 40 / 14 us;
+// n = 16, 64 rows, 1024 -> 1024 9.4 / 14.  Returns the bytes of the parts.
 size_t split_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass pass, int32_t dtype,
                     gasloc::LinearArgs* a) {
   const int n = c.n;
   const int64_t total = a->tiles.begin[n], want = 2 * static_cast<int64_t>(c.cus);
   if (total == 0 || total >= want) return 0;
   const int64_t per_step = gasloc::kLinearStep / static_cast<int64_t>(param_bytes(dtype));
-  int64_t tiles[gasloc::kMaxReplicas], steps[gasloc::kMaxReplicas], work = 0;
+  int64_t tiles[gasloc::kMaxReplicas], steps[gasloc::kMaxReplicas], work = 0, longest = 0;
   for (int i = 0; i < n; ++i) {
-    const int w = a->order[i];
-    const int64_t depth = pass == gasloc::kLinearForward ? a->in_features
-                          : pass == gasloc::kLinearInput ? a->out_features
-                                                         : row_ptr[w + 1] - row_ptr[w];
     tiles[i] = a->tiles.begin[i + 1] - a->tiles.begin[i];
-    steps[i] = (depth + per_step - 1) / per_step;
+    steps[i] = (depth_of(*a, row_ptr, pass, a->order[i]) + per_step - 1) / per_step;
     work += tiles[i] * steps[i];
+    if (tiles[i] > 0) longest = std::max(longest, steps[i]);
   }
-  const int64_t wide = pass == gasloc::kLinearForward ? a->out_features : a->in_features;
-  const int64_t tall = pass == gasloc::kLinearWeight ? static_cast<int64_t>(n) * a->out_features : row_ptr[n];
-  const int64_t outputs = tall * wide / total;  // per tile
-  int64_t part = std::max<int64_t>({4, 16 * outputs / (128 * 128), (work + want - 1) / want});
-  part = (part + 3) / 4 * 4;
-  bool any = false;
-  for (int i = 0; i < n; ++i) any = any || (tiles[i] > 0 && steps[i] > part);
-  if (!any) return 0;
+  const int64_t part = std::max<int64_t>(4, ((work + want - 1) / want + 3) / 4 * 4);
+  const auto parts_of = [&](int i) { return std::max<int64_t>(1, (steps[i] + part - 1) / part); };
+  int64_t all_parts = 0;
+  for (int i = 0; i < n; ++i) all_parts += parts_of(i);
+  const int64_t outputs = outputs_of(n, *a, row_ptr, pass);
+  const size_t bytes = sizeof(float) * static_cast<size_t>(pass == gasloc::kLinearWeight ? outputs / n * all_parts
+                                                                                          : outputs * parts_of(0));
+  if (longest - part < 16 + 2 * static_cast<int64_t>(bytes >> 20)) return 0;
   a->chunk = static_cast<int32_t>(part * per_step);
-  size_t values = 0;
   for (int i = 0; i < n; ++i) {
-    const int64_t parts = std::max<int64_t>(1, (steps[i] + part - 1) / part);
-    a->tiles.begin[i + 1] = static_cast<int32_t>(a->tiles.begin[i] + tiles[i] * parts);
-    a->parts.begin[i + 1] = static_cast<int32_t>(a->parts.begin[i] + parts);
+    a->tiles.begin[i + 1] = static_cast<int32_t>(a->tiles.begin[i] + tiles[i] * parts_of(i));
+    a->parts.begin[i + 1] = static_cast<int32_t>(a->parts.begin[i] + parts_of(i));
   }
-  if (pass == gasloc::kLinearWeight)
-    values = static_cast<size_t>(a->parts.begin[n]) * a->out_features * a->in_features;
-  else
-    values = static_cast<size_t>(a->parts.begin[1]) * row_ptr[n] *
-             (pass == gasloc::kLinearForward ? a->out_features : a->in_features);
-  return sizeof(float) * values;
+  return bytes;
 }
 
 gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPass pass, const int64_t* row_ptr,
@@ -304,13 +326,13 @@ gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPas
   // each, 2048 -> 2048, bf16 rows, fp32 weights: 61 us against 48).
   if (pass == gasloc::kLinearForward && most <= gasloc::kFewRows) tile = gasloc::kFewRows;
   bool fits = linear_tiles(c->n, row_ptr, pass, tile, a);
-  if (fits && tile == 256 && a->tiles.begin[c->n] < 2 * c->cus) {
-    tile = 128;
-    fits = linear_tiles(c->n, row_ptr, pass, tile, a);
+  if (tile == 128 || (fits && tile == 256 && a->tiles.begin[c->n] < 2 * c->cus)) {
+    tile = cut_linear(*c, row_ptr, pass, dtype, a);
+    fits = tile != 0;
   }
   if (!fits) return fail(c, GASLOC_EINVAL, "product too large for one launch");
   if (a->tiles.begin[c->n] == 0) return GASLOC_OK;
-  if (tile == 128) {
+  if (tile == 128 || tile == 64) {
     CHECK(c, check_workspace(workspace, workspace_bytes, split_linear(*c, row_ptr, pass, dtype, a)));
     a->partial = static_cast<float*>(workspace);
   }
@@ -604,7 +626,7 @@ gasloc_status gasloc_linear_workspace(const gasloc_ctx* c, int32_t out_features,
       gasloc::LinearArgs a{};
       a.out_features = out_features;
       a.in_features = in_features;
-      if (linear_tiles(c->n, row_ptr, pass, 128, &a))
+      if (cut_linear(*c, row_ptr, pass, dtype, &a) != 0)
         *bytes = std::max(*bytes, split_linear(*c, row_ptr, pass, dtype, &a));
     }
     *bytes = round256(*bytes);

@@ -158,7 +158,7 @@ struct LinearArgs {
 };
 constexpr int kLinearStep = 64;  // bytes of k per step; the kernel takes four at a time
 constexpr int kFewRows = 16;
-// tile: rows and columns of a workgroup's part of C (256, or 128: always 128 without vec and in F32; kFewRows:
+// tile: rows and columns of a workgroup's part of C (256, 128 or 64; 256 only with vec and in BF16; kFewRows:
 // forward pass of workers with at most so many rows, 16 outputs of all of them per workgroup).  vec: every row of
 // either operand, of C and of the gradients begins on a 16-byte boundary and is a whole number of 16-byte chunks
 // of activations.

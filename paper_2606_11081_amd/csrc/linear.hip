@@ -3,7 +3,7 @@
 // all of the form C[m][n] = sum_k A(m, k) B(n, k).
 //
 // A workgroup makes one tile of C: 256 x 256 outputs by eight waves (bf16), or
-// 128 x 128 by four; 64 bytes of k of both operands at a time (a step) pass
+// 128 x 128 or 64 x 64 by four; 64 bytes of k of both operands at a time (a step) pass
 // through four buffers in LDS, with the loads of what follows in flight in
 // registers (fp32 weights that meet bf16 activations are rounded on the way).
 // An operand whose rows run along k lies in LDS as [row][k] and is read in
@@ -12,7 +12,9 @@
 //
 // Measured, bf16 rows: n = 16, 32768 rows, 1024 -> 4096, bf16 weights 270 us
 // (1020 TFLOP/s); input gradient of 2048 -> 2048 under fp32 weights 264 us (1040);
-// weight gradient of n = 8, 30011 ragged rows 227 us (1110).  A 2048-deep loop
+// weight gradient of n = 8, 30011 ragged rows 227 us (1110).  Small products wait
+// for their first loads and the launches: n = 8, 256 rows each, 1024 -> 1024 in bf16
+// 11 us; weight gradient of n = 3, 1111 rows, 513 x 257 in fp32 16 us, in two launches.  A 2048-deep loop
 // alone runs at 1100 to 1200.  The loads bound it: without those of the loop it
 // ran at 1340 to 1510, with all of them hitting L2 at 1230 to 1330, while the
 // place of stores, loads and waits among the products changes less than 2%.  A
@@ -169,13 +171,16 @@ struct Operand {
     else
       return lds + g * 4 * kStride + (row + i) * 4;
   }
-  // How the 32-byte blocks of line k are permuted.
-  __device__ __forceinline__ static int across(int k) { return k % 4 + k / 8 % 2 * 4; }
+  // How the 32-byte blocks of line k are permuted (of a line of 64 rows there are four).
+  __device__ __forceinline__ static int across(int k) {
+    return ROWS == 64 ? k % 4 ^ k / 8 % 2 : k % 4 + k / 8 % 2 * 4;
+  }
 
   __device__ __forceinline__ void store(uint32_t to, int j, const Words& words) const {
     static_assert(!KC || kLines % 16 == 0, "a thread's rows are permuted alike");
     static_assert(KC || CT != GASLOC_BF16 || kLines % 8 == 0, "or by turns");
     // line k + 8 has its blocks exchanged by fours
+    static_assert(KC || CT != GASLOC_BF16 || ROWS >= 128 || kLines % 16 == 0, "lines of 128 bytes stay as they are");
     if (!KC && CT == GASLOC_BF16 && kLines * j / 8 % 2 == 1) to ^= 128;
     to += j * kLines * kStride;
     if constexpr (ST == CT) {
@@ -545,6 +550,17 @@ __global__ __launch_bounds__(256) void k_linear_rows(LinearArgs a) {
   if (n < N) store_row<AT, 4>(a.out, (r0 + lane % 16) * a.out_ld + n, N - n, o);
 }
 
+// Tiles of four waves, whose sums may be split.
+template <int PASS, int PT, int AT, int TILE, int WAVES_M, int WAVES_N>
+hipError_t launch_small(const LinearArgs& a, bool vec, hipStream_t stream) {
+  const bool split = a.chunk != 0;
+  return launch_kernel(vec ? split ? k_linear<PASS, PT, AT, TILE, TILE, WAVES_M, WAVES_N, true, true>
+                                   : k_linear<PASS, PT, AT, TILE, TILE, WAVES_M, WAVES_N, true, false>
+                       : split ? k_linear<PASS, PT, AT, TILE, TILE, WAVES_M, WAVES_N, false, true>
+                               : k_linear<PASS, PT, AT, TILE, TILE, WAVES_M, WAVES_N, false, false>,
+                       dim3(a.tiles.begin[a.n]), 256, 0, stream, a);
+}
+
 template <int PASS, int PT, int AT>
 hipError_t launch_types(const LinearArgs& a, int tile, bool vec, hipStream_t stream) {
   const dim3 grid(a.tiles.begin[a.n]);
@@ -555,14 +571,9 @@ hipError_t launch_types(const LinearArgs& a, int tile, bool vec, hipStream_t str
   if constexpr (PASS == kLinearForward) {
     if (tile == kFewRows) return launch_kernel(k_linear_rows<PT, AT>, grid, 256, 0, stream, a);
   }
-  if (a.chunk == 0)
-    return launch_kernel(vec ? k_linear<PASS, PT, AT, 128, 128, 2, 2, true, false>
-                             : k_linear<PASS, PT, AT, 128, 128, 2, 2, false, false>,
-                         grid, 256, 0, stream, a);
-  const hipError_t e = launch_kernel(vec ? k_linear<PASS, PT, AT, 128, 128, 2, 2, true, true>
-                                         : k_linear<PASS, PT, AT, 128, 128, 2, 2, false, true>,
-                                     grid, 256, 0, stream, a);
-  if (e != hipSuccess) return e;
+  const hipError_t e = tile == 64 ? launch_small<PASS, PT, AT, 64, 1, 4>(a, vec, stream)
+                                  : launch_small<PASS, PT, AT, 128, 2, 2>(a, vec, stream);
+  if (e != hipSuccess || a.chunk == 0) return e;
   const int N = PASS == kLinearForward ? a.out_features : a.in_features;
   const int64_t all = static_cast<int64_t>(PASS == kLinearWeight ? a.out_features : a.rows.begin[a.n]) * N;
   const dim3 join(static_cast<unsigned>(all / 256 < 2048 ? (all + 255) / 256 : 2048), PASS == kLinearWeight ? a.n : 1);

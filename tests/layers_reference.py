@@ -115,3 +115,15 @@ def linear_grad_weight(x, dout, row_ptr):
         out[i] = dout[a:b].T @ x[a:b]
         e[i] = 2 * (b - a + 4) * U * (np.abs(dout[a:b]).T @ np.abs(x[a:b]))
     return out, e + TINY
+
+
+# Products whose tiles are 128 outputs a side, on 256 CUs: with many outputs, and with sums long enough to be split.
+# (pass, split) -> row_ptr, out_features, in_features
+LARGE = {
+    ("linear", False): ([0, 1400, 2100], 4104, 72),
+    ("linear_grad_input", False): ([0, 1400, 2100], 72, 4104),
+    ("linear_grad_weight", False): ([0, 50, 77], 2056, 2064),
+    ("linear", True): ([0, 400, 528], 264, 72_008),
+    ("linear_grad_input", True): ([0, 400, 528], 72_008, 264),
+    ("linear_grad_weight", True): ([0, 50_011, 80_000], 264, 520),
+}

@@ -429,6 +429,32 @@ def test_linear_long_sums(kind, params, act):
     assert np.array_equal(got, ref.to_bf16(want) if act == "bf16" else want)
 
 
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("params,act", TYPES)
+@pytest.mark.parametrize("kind,split", ref.LARGE)
+def test_linear_large_tiles(kind, split, params, act, odd):
+    """Tiles of 128 outputs, whole and in parts; odd: sizes and columns that no vector fits.  Whole numbers, whose
+    sums (at most 4 * 80000) are exact."""
+    say("large", kind, split, params, act, odd)
+    ptr, m, k = ref.LARGE[kind, split]
+    ptr, rows, m, k, begin = np.array(ptr), ptr[-1], m - odd, k - odd, int(odd)
+    r = Rows(2, m * k, begin, params, stepped=[0, 1])
+    w = r.put(integers(1, -2, 2, 2, m * k)).reshape(2, m, k)
+    x, xs, _ = rows_of(integers(2, -2, 2, rows, k), act)
+    dout, d, _ = rows_of(integers(3, -2, 2, rows, m), act)
+    if kind == "linear":
+        got, want = r.run.linear(begin, m, k, x, ptr)[:rows].double().cpu().numpy(), ref.linear(w, xs, ptr, act)[0]
+    elif kind == "linear_grad_input":
+        got = r.run.linear_grad_input(begin, m, k, dout, ptr)[:rows].double().cpu().numpy()
+        want = ref.linear_grad_input(w, d, ptr, act)[0]
+    else:
+        r.run.linear_grad_weight(begin, m, k, x, dout, ptr, r.grads, accumulate=odd)
+        got, want = r.gradient(), ref.linear_grad_weight(xs, d, ptr)[0].reshape(2, -1) + 7.0 * odd
+        assert np.array_equal(got, want)
+        return
+    assert np.array_equal(got, ref.to_bf16(want) if act == "bf16" else want)
+
+
 def test_linear_infinities_and_nan_stay_in_their_rows():
     """What is not finite in one worker's rows, or in the rows behind a ragged end, reaches no other worker."""
     import torch

@@ -11,6 +11,7 @@ import numpy as np
 import pytest
 
 import paper_2606_11081_amd as g
+from tests import layers_reference as ref
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
@@ -245,6 +246,26 @@ def random_rows(rng, n):
     return rp(*rows)
 
 
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("odd", [0, 1])
+@pytest.mark.parametrize("kind,split", ref.LARGE)
+def test_large_products_take_large_tiles(shim, kind, split, odd, act):
+    """The cases that the GPU tests mean for tiles of 128 are such, in parts or not."""
+    ptr, m, k = ref.LARGE[kind, split]
+    m, k, ptr = m - odd, k - odd, np.array(ptr, np.int64)
+    ctx = Context(shim, n=2, P=m * k + 8, dtype=F32)
+    size = ctypes.c_size_t()
+    assert shim.gasloc_linear_workspace(ctx.c, m, k, ptr.ctypes.data, act, ctypes.byref(size)) == OK
+    changes = dict(weight=0, out_features=m, in_features=k, workspace_bytes=size.value)
+    for key in calls(ptr)["gasloc_" + kind]:
+        changes.update({"x_ld": dict(x_ld=k), "dx_ld": dict(dx_ld=k), "out_ld": dict(out_ld=m),
+                        "dout_ld": dict(dout_ld=m), "grad_ld": dict(grad_ld=(m * k + 11) // 4 * 4)}.get(key, {}))
+    assert call(ctx, "gasloc_" + kind, ptr=ptr, act=act, **changes) == OK, shim.shim_error()
+    plan = np.zeros(3 + 3 * 2 + 2, np.int64)
+    shim.shim_linear_plan(2, plan.ctypes.data_as(ctypes.c_void_p))
+    assert plan[0] == 128 and bool(plan[1]) == (not odd) and (plan[2] > 0) == split
+
+
 @pytest.mark.parametrize("seed", range(60))
 def test_linear_plans_cover_every_product_once(shim, seed):
     """Tiles of each worker times its parts, the parts long enough for the sums, and the workspace that the size
@@ -272,7 +293,7 @@ def test_linear_plans_cover_every_product_once(shim, seed):
         tile, vec, chunk = (int(v) for v in plan[:3])
         starts, parts, order = plan[3:4 + n], plan[4 + n:5 + 2 * n], plan[5 + 2 * n:]
         assert sorted(order) == list(range(n))
-        assert tile in (16, 128, 256) and (tile != 256 or (vec and act == BF16))
+        assert tile in (16, 64, 128, 256) and (tile != 256 or (vec and act == BF16))
         step = 32 if act == BF16 else 16
         assert chunk % (4 * step) == 0
         used = 0
