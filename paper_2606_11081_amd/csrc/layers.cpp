@@ -258,6 +258,16 @@ int64_t outputs_of(int n, const gasloc::LinearArgs& a, const int64_t* row_ptr, g
                                        : row_ptr[n] * (pass == gasloc::kLinearForward ? a.out_features : a.in_features);
 }
 
+// Whether a product in bf16 takes less time in `large` tiles of 256 than in `small` ones of 128.  The first fill a CU
+// each, of the second two go on a CU: a round of large tiles takes 1.65 times as long as one of pairs of small ones,
+// which takes 1/0.65 times as long as one of single ones.  Asked below two rounds of large tiles, which are taken from
+// there on (they read half as much).  1024 -> 1024, n = 8, large /
+// small tiles: 2048 rows each (256 / 1024 tiles) 34 / 41 us, 1024 rows (128 / 512) 29 / 23.
+bool large_tiles(const gasloc_ctx& c, int64_t large, int64_t small) {
+  const int64_t rounds = (large + c.cus - 1) / c.cus, per_cu = (small + c.cus - 1) / c.cus;
+  return 33 * rounds <= 20 * (per_cu / 2) + 13 * (per_cu % 2);
+}
+
 // Cuts a product that tiles of 256 do not suit into tiles of 128 outputs, or of 64 where those would be too few for
 // the CUs (fewer than one per CU, or two in F32, whose matrix instructions take longer) and none would have many steps
 // to do (20 per CU in BF16, 128 in F32): such products wait for their loads, not for the matrix cores.  Others keep the
@@ -326,7 +336,15 @@ gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPas
   // each, 2048 -> 2048, bf16 rows, fp32 weights: 61 us against 48).
   if (pass == gasloc::kLinearForward && most <= gasloc::kFewRows) tile = gasloc::kFewRows;
   bool fits = linear_tiles(c->n, row_ptr, pass, tile, a);
-  if (tile == 128 || (fits && tile == 256 && a->tiles.begin[c->n] < 2 * c->cus)) {
+  const int64_t large = a->tiles.begin[c->n];
+  if (tile == 256 && fits && large < 2 * c->cus) {
+    linear_tiles(c->n, row_ptr, pass, 128, a);
+    if (large_tiles(*c, large, a->tiles.begin[c->n]))
+      linear_tiles(c->n, row_ptr, pass, 256, a);
+    else
+      tile = 128;
+  }
+  if (tile == 128) {
     tile = cut_linear(*c, row_ptr, pass, dtype, a);
     fits = tile != 0;
   }

@@ -118,12 +118,16 @@ def linear_grad_weight(x, dout, row_ptr):
 
 
 # Products whose tiles are 128 outputs a side, on 256 CUs: with many outputs, and with sums long enough to be split.
-# (pass, split) -> row_ptr, out_features, in_features
+# (pass, activations, split) -> row_ptr, out_features, in_features
 LARGE = {
-    ("linear", False): ([0, 1400, 2100], 4104, 72),
-    ("linear_grad_input", False): ([0, 1400, 2100], 72, 4104),
-    ("linear_grad_weight", False): ([0, 50, 77], 2056, 2064),
-    ("linear", True): ([0, 400, 528], 264, 72_008),
-    ("linear_grad_input", True): ([0, 400, 528], 72_008, 264),
-    ("linear_grad_weight", True): ([0, 50_011, 80_000], 264, 520),
+    ("linear", "f32", False): ([0, 1400, 2100], 4104, 72),
+    ("linear", "bf16", False): ([0, 700, 1100], 4104, 72),
+    ("linear_grad_input", "f32", False): ([0, 1400, 2100], 72, 4104),
+    ("linear_grad_input", "bf16", False): ([0, 700, 1100], 72, 4104),
+    ("linear_grad_weight", "f32", False): ([0, 50, 77], 2056, 2064),
+    ("linear_grad_weight", "bf16", False): ([0, 50, 77], 2056, 1032),
 }
+for _act in ("f32", "bf16"):
+    LARGE["linear", _act, True] = ([0, 400, 528], 264, 72_008)
+    LARGE["linear_grad_input", _act, True] = ([0, 400, 528], 72_008, 264)
+    LARGE["linear_grad_weight", _act, True] = ([0, 50_011, 80_000], 264, 520)

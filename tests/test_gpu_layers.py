@@ -430,13 +430,12 @@ def test_linear_long_sums(kind, params, act):
 
 
 @pytest.mark.parametrize("odd", [False, True])
-@pytest.mark.parametrize("params,act", TYPES)
-@pytest.mark.parametrize("kind,split", ref.LARGE)
-def test_linear_large_tiles(kind, split, params, act, odd):
+@pytest.mark.parametrize("kind,params,act,split", [(k, p, a, s) for k, a, s in ref.LARGE for p, b in TYPES if a == b])
+def test_linear_large_tiles(kind, params, act, split, odd):
     """Tiles of 128 outputs, whole and in parts; odd: sizes and columns that no vector fits.  Whole numbers, whose
     sums (at most 4 * 80000) are exact."""
-    say("large", kind, split, params, act, odd)
-    ptr, m, k = ref.LARGE[kind, split]
+    say("large", kind, params, act, split, odd)
+    ptr, m, k = ref.LARGE[kind, act, split]
     ptr, rows, m, k, begin = np.array(ptr), ptr[-1], m - odd, k - odd, int(odd)
     r = Rows(2, m * k, begin, params, stepped=[0, 1])
     w = r.put(integers(1, -2, 2, 2, m * k)).reshape(2, m, k)

@@ -246,13 +246,12 @@ def random_rows(rng, n):
     return rp(*rows)
 
 
-@pytest.mark.parametrize("act", [F32, BF16])
 @pytest.mark.parametrize("odd", [0, 1])
-@pytest.mark.parametrize("kind,split", ref.LARGE)
-def test_large_products_take_large_tiles(shim, kind, split, odd, act):
+@pytest.mark.parametrize("kind,act,split", ref.LARGE)
+def test_large_products_take_large_tiles(shim, kind, act, split, odd):
     """The cases that the GPU tests mean for tiles of 128 are such, in parts or not."""
-    ptr, m, k = ref.LARGE[kind, split]
-    m, k, ptr = m - odd, k - odd, np.array(ptr, np.int64)
+    ptr, m, k = ref.LARGE[kind, act, split]
+    m, k, ptr, act = m - odd, k - odd, np.array(ptr, np.int64), F32 if act == "f32" else BF16
     ctx = Context(shim, n=2, P=m * k + 8, dtype=F32)
     size = ctypes.c_size_t()
     assert shim.gasloc_linear_workspace(ctx.c, m, k, ptr.ctypes.data, act, ctypes.byref(size)) == OK
