@@ -227,7 +227,7 @@ __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c) {
 // A tile of TM x TN outputs by WAVES_M x WAVES_N waves.  SPLIT: a workgroup takes `chunk` of k, and where a worker
 // has several such parts it leaves its sums in `partial` for the join.
 template <int PASS, int PT, int AT, int TM, int TN, int WAVES_M, int WAVES_N, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a) {
+__global__ __launch_bounds__(kWave* WAVES_M* WAVES_N, 2) void k_linear(LinearArgs a) {
   constexpr int THREADS = kWave * WAVES_M * WAVES_N;
   constexpr bool kForward = PASS == kLinearForward, kWeight = PASS == kLinearWeight;
   using OpA = Operand<TM, THREADS, !kWeight, AT, AT, VEC>;
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
   // through the wave's own part of LDS, so that whole lines are stored.
   using Out = typename std::conditional<kWeight || AT == GASLOC_F32 || SPLIT, float, uint16_t>::type;
   constexpr int kOutStride = WN * static_cast<int>(sizeof(Out)) + 16;
-  constexpr int V = VEC ? 16 / static_cast<int>(sizeof(Out)) : 1;
+  constexpr int V = 16 / static_cast<int>(sizeof(Out));
   static_assert(THREADS / kWave * 16 * kOutStride <= kBuffers * (OpA::kLds + OpB::kLds),
                 "sixteen rows of every wave fit");
   char* const mine = s_tiles + wave * 16 * kOutStride;
@@ -431,12 +431,24 @@ __global__ __launch_bounds__(kWave* WAVES_M* WAVES_N) void k_linear(LinearArgs a
         *reinterpret_cast<f32x4*>(to) = v;
       } else if constexpr (VEC) {
         *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(from);
+      } else if (n + V <= N) {  // at the alignment of an element
+        u32x4 v = *reinterpret_cast<const u32x4*>(from);
+        if constexpr (kWeight) {
+          if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, load_words4<false>(to)) +
+                                                     __builtin_bit_cast(f32x4, v));
+        }
+        *reinterpret_cast<u32x4_any*>(to) = v;
       } else {
-        const Out v = *reinterpret_cast<const Out*>(from);
-        if constexpr (kWeight)
-          *to = add ? *to + v : v;
-        else
-          *to = v;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          if (n + q < N) {
+            const Out v = reinterpret_cast<const Out*>(from)[q];
+            if constexpr (kWeight)
+              to[q] = add ? to[q] + v : v;
+            else
+              to[q] = v;
+          }
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
