@@ -613,14 +613,20 @@ class GASLoC:
             return torch.empty((rows, cols), dtype=dtype, device=device), cols
         return t, _rows_of(name, t, rows, cols, dtype, device)
 
-    def _workspace(self, workspace, need, device):
+    def _workspace(self, workspace, device, name, *args):
+        """(tensors that hold the workspace, its address, its bytes): the one given, or one of the size that the
+        library's call `name` wants."""
         import torch
 
         if workspace is None:
-            return torch.empty(need, dtype=torch.uint8, device=device), need
-        if workspace.device != device or not workspace.is_contiguous():
+            need = ctypes.c_size_t()
+            _check(getattr(library(), name)(self.ctx, *args, ctypes.byref(need)))
+            if need.value == 0:
+                return (), None, 0
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+        elif workspace.device != device or not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous on %s" % device)
-        return workspace, workspace.numel() * workspace.element_size()
+        return (workspace,), workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
     def _tokens(self, tokens, rows, device):
         import torch
@@ -655,7 +661,7 @@ class GASLoC:
         out, ld = self._out("out", out, rows, width, torch.bfloat16 if code == GASLOC_BF16 else torch.float32, device)
         self._tokens(tokens, rows, device)
         self._run("gasloc_embedding", (tokens, out), int(table), int(vocab), int(width), float(scale),
-                  rp.ctypes.data, tokens.data_ptr(), code, out.data_ptr(), ld)
+                  rp.tobytes(), tokens.data_ptr(), code, out.data_ptr(), ld)
         return out
 
     def embedding_grad(self, table, vocab, width, tokens, row_ptr, dout, grads, scale=1.0, accumulate=False,
@@ -665,10 +671,11 @@ class GASLoC:
         ld = _rows_of("dout", dout, rows, width, dout.dtype, device)
         gld = self._grads(grads, device)
         self._tokens(tokens, rows, device)
-        ws, size = self._workspace(workspace, gasloc_embedding_grad_workspace(self.ctx, width, rp), device)
-        self._run("gasloc_embedding_grad", (tokens, dout, grads, ws), int(table), int(vocab), int(width), float(scale),
-                  rp.ctypes.data, tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld, grads.data_ptr(), gld,
-                  bool(accumulate), ws.data_ptr(), size)
+        kept, ws, size = self._workspace(workspace, device, "gasloc_embedding_grad_workspace", int(width),
+                                         rp.tobytes())
+        self._run("gasloc_embedding_grad", (tokens, dout, grads, *kept), int(table), int(vocab), int(width), float(scale),
+                  rp.tobytes(), tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld, grads.data_ptr(), gld,
+                  bool(accumulate), ws, size)
 
     def layer_norm(self, gain, bias, width, x, row_ptr, eps=1e-5, out=None, stats=None):
         """(out, stats): the normalised rows (gain and bias at these columns; bias None: none) and every
@@ -678,7 +685,7 @@ class GASLoC:
         out, ld = self._out("out", out, rows, width, x.dtype, device)
         stats = self._stats(stats, rows, device)
         self._run("gasloc_layer_norm", (x, out, stats), int(gain), -1 if bias is None else int(bias), int(width),
-                  float(eps), rp.ctypes.data, x.data_ptr(), x_ld, _act(x.dtype), out.data_ptr(), ld, stats.data_ptr())
+                  float(eps), rp.tobytes(), x.data_ptr(), x_ld, _act(x.dtype), out.data_ptr(), ld, stats.data_ptr())
         return out, stats
 
     def layer_norm_grad(self, gain, bias, width, x, row_ptr, stats, dout, grads, dx=None, accumulate=False,
@@ -693,25 +700,26 @@ class GASLoC:
             raise ValueError("stats: those that layer_norm returned")
         stats = self._stats(stats, rows, device)
         gld = self._grads(grads, device)
-        ws, size = self._workspace(workspace, gasloc_layer_norm_grad_workspace(self.ctx, width, rp), device)
-        self._run("gasloc_layer_norm_grad", (x, stats, dout, dx, grads, ws), int(gain),
-                  -1 if bias is None else int(bias), int(width), rp.ctypes.data, x.data_ptr(), x_ld, stats.data_ptr(),
+        kept, ws, size = self._workspace(workspace, device, "gasloc_layer_norm_grad_workspace", int(width),
+                                         rp.tobytes())
+        self._run("gasloc_layer_norm_grad", (x, stats, dout, dx, grads, *kept), int(gain),
+                  -1 if bias is None else int(bias), int(width), rp.tobytes(), x.data_ptr(), x_ld, stats.data_ptr(),
                   dout.data_ptr(), d_ld, _act(x.dtype), dx.data_ptr(), ld, grads.data_ptr(), gld, bool(accumulate),
-                  ws.data_ptr(), size)
+                  ws, size)
         return dx
 
     def _linear_workspace(self, workspace, out_features, in_features, rp, dtype, device):
-        need = 0 if workspace is not None else gasloc_linear_workspace(self.ctx, out_features, in_features, rp, dtype)
-        return self._workspace(workspace, need, device)
+        return self._workspace(workspace, device, "gasloc_linear_workspace", int(out_features), int(in_features),
+                               rp.tobytes(), _act(dtype))
 
     def linear(self, weight, out_features, in_features, x, row_ptr, out=None, workspace=None):
         """out[t] = W_i x[t], W_i the [out_features, in_features] matrix at column `weight` of worker i's row."""
         rp, rows, device = self._layer(row_ptr)
         x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
         out, ld = self._out("out", out, rows, out_features, x.dtype, device)
-        ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
-        self._run("gasloc_linear", (x, out, ws), int(weight), int(out_features), int(in_features),
-                  rp.ctypes.data, x.data_ptr(), x_ld, _act(x.dtype), out.data_ptr(), ld, ws.data_ptr(), size)
+        kept, ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
+        self._run("gasloc_linear", (x, out, *kept), int(weight), int(out_features), int(in_features),
+                  rp.tobytes(), x.data_ptr(), x_ld, _act(x.dtype), out.data_ptr(), ld, ws, size)
         return out
 
     def linear_grad_input(self, weight, out_features, in_features, dout, row_ptr, dx=None, workspace=None):
@@ -719,9 +727,9 @@ class GASLoC:
         rp, rows, device = self._layer(row_ptr)
         d_ld = _rows_of("dout", dout, rows, out_features, dout.dtype, device)
         dx, ld = self._out("dx", dx, rows, in_features, dout.dtype, device)
-        ws, size = self._linear_workspace(workspace, out_features, in_features, rp, dout.dtype, device)
-        self._run("gasloc_linear_grad_input", (dout, dx, ws), int(weight), int(out_features), int(in_features),
-                  rp.ctypes.data, dout.data_ptr(), d_ld, _act(dout.dtype), dx.data_ptr(), ld, ws.data_ptr(), size)
+        kept, ws, size = self._linear_workspace(workspace, out_features, in_features, rp, dout.dtype, device)
+        self._run("gasloc_linear_grad_input", (dout, dx, *kept), int(weight), int(out_features), int(in_features),
+                  rp.tobytes(), dout.data_ptr(), d_ld, _act(dout.dtype), dx.data_ptr(), ld, ws, size)
         return dx
 
     def linear_grad_weight(self, weight, out_features, in_features, x, dout, row_ptr, grads, accumulate=False,
@@ -731,10 +739,10 @@ class GASLoC:
         x_ld = _rows_of("x", x, rows, in_features, x.dtype, device)
         d_ld = _rows_of("dout", dout, rows, out_features, x.dtype, device)
         gld = self._grads(grads, device)
-        ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
-        self._run("gasloc_linear_grad_weight", (x, dout, grads, ws), int(weight), int(out_features), int(in_features),
-                  rp.ctypes.data, x.data_ptr(), x_ld, dout.data_ptr(), d_ld, _act(x.dtype), grads.data_ptr(), gld,
-                  bool(accumulate), ws.data_ptr(), size)
+        kept, ws, size = self._linear_workspace(workspace, out_features, in_features, rp, x.dtype, device)
+        self._run("gasloc_linear_grad_weight", (x, dout, grads, *kept), int(weight), int(out_features), int(in_features),
+                  rp.tobytes(), x.data_ptr(), x_ld, dout.data_ptr(), d_ld, _act(x.dtype), grads.data_ptr(), gld,
+                  bool(accumulate), ws, size)
 
     def counters(self):
         """(k, stepped, rounds_done): per-worker AdamW step counts, which workers
