@@ -106,12 +106,17 @@ struct Operand {
   struct Load {
     __amdgpu_buffer_rsrc_t w;
     int lines, limit;  // lines and columns inside
+    int alone;         // lines from here on end inside a chunk that nothing may be read behind
   };
   // The memory of the next load; `at` moves on.  Behind the last step nothing is inside.
   __device__ __forceinline__ Load next() {
     const int inside = max(0, min(left, KT));
-    const uint32_t bytes = KC ? full : full - static_cast<uint32_t>(KT - inside) * line;
-    const Load l{window(at, left > 0 ? bytes : 0), KC ? rows : inside, KC ? left : rows};
+    // Columns behind the rows of the tile meet no output that is stored: where a line follows in memory, the chunk
+    // that goes over a line's end is read as a whole.
+    const bool follows = !KC && !VEC && left > KT && line >= 16;
+    const uint32_t bytes = KC ? full : full - static_cast<uint32_t>(KT - inside) * line + (follows ? 16 : 0);
+    const Load l{window(at, left > 0 ? bytes : 0), KC ? rows : inside, KC ? left : rows,
+                 KC || line < 16 ? 0 : follows ? KT : inside - 1};
     if (KC) full -= kSpan * KT * kSrc;
     at += ahead;
     left -= kSpan * KT;
@@ -129,18 +134,20 @@ struct Operand {
       for (int e = 0; e < 4; ++e) words[j][e] = v[e];
     } else {
       // Whole chunks at the alignment of an element, which the memory instructions take; the one that goes over the
-      // end of a line by elements.
-      const bool in_line = line_of(j) < l.lines;
+      // end of a line by elements, if nothing may be read there or (along k) it has to be zero.
+      const bool in_line = line_of(j) < l.lines, alone = line_of(j) >= l.alone;
+      const bool split = col < l.limit && col + E > l.limit && alone;
       const uint32_t o = off + down;
       const u32x4 v = __builtin_bit_cast(
-          u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.w, in_line && col + E <= l.limit ? o : kNowhere, 0, 0));
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(l.w, in_line && col < l.limit && !split ? o : kNowhere, 0, 0));
 #pragma unroll
       for (int e = 0; e < 4; ++e) words[j][e] = v[e];
-      if (in_line && col < l.limit && col + E > l.limit) {
-        uint32_t e[E];
+      if (in_line && split) {
+        uint32_t e[E], here = o;
+        asm volatile("" : "+v"(here));  // the elements' offsets are made here, not kept in registers through the loop
 #pragma unroll
         for (int q = 0; q < E; ++q) {
-          const uint32_t at_q = col + q < l.limit ? o + q * kSrc : kNowhere;
+          const uint32_t at_q = col + q < l.limit ? here + q * kSrc : kNowhere;
           if constexpr (ST == GASLOC_BF16)
             e[q] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(l.w, at_q, 0, 0));
           else
