@@ -239,19 +239,23 @@ __global__ __launch_bounds__(256) void k_embedding_sums(EmbeddingGradArgs a) {
     __syncthreads();
     for (int64_t e = lo + tid; e < hi; e += threads) s_key[a.keys[e] - static_cast<uint32_t>(k0)] = 1;
     __syncthreads();
-    // vectors on their boundaries, whatever the row's: a row of odd width begins inside one
+    // Rows that follow each other are one stretch of memory.  Vectors on their boundaries, whatever the row's: a row
+    // of odd width begins inside one.
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = k0; k < k1; ++k) {
+    for (int k = k0, stop; k < k1; k = stop) {
+      stop = k + 1;
       if (s_key[k - k0]) continue;
+      while (stop < k1 && !s_key[stop - k0]) ++stop;
+      const int cols = (stop - k) * a.width;
       float* g = a.grads + static_cast<int64_t>(i) * a.grad_ld + a.begin + static_cast<int64_t>(k) * a.width;
       const int inside = static_cast<int>(reinterpret_cast<uintptr_t>(g) / 4 % 4);
-      for (int c = tid * V - inside; c < a.width; c += threads * V) {
-        if (c >= 0 && c + V <= a.width) {
+      for (int c = tid * V - inside; c < cols; c += threads * V) {
+        if (c >= 0 && c + V <= cols) {
           st_stream(reinterpret_cast<f32x4*>(g + c), zero);
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            if (c + e >= 0 && c + e < a.width) g[c + e] = 0.0f;
+            if (c + e >= 0 && c + e < cols) g[c + e] = 0.0f;
         }
       }
     }
