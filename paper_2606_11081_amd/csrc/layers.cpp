@@ -273,7 +273,7 @@ bool large_tiles(const gasloc_ctx& c, int64_t large, int64_t small) {
 // to do (20 per CU in BF16, 128 in F32): such products wait for their loads, not for the matrix cores.  Others keep the
 // tiles of 128, which read half as much for an output.  Tiles of 128 / of 64, bf16: n = 4, 256 rows each, 512 -> 512
 // 7.9 / 5.4 us; n = 16, 512 rows, 512 -> 512 9.2 / 11.7; the weight's gradient of n = 4, 4096 rows, 512 -> 512 25 / 29;
-// fp32: n = 4, 600 rows, 1024 -> 2560 212 / 119.  Returns the side, 0 if the product is too large.
+// fp32: n = 4, 256 rows, 512 -> 512 35 / 13.  Returns the side, 0 if the product is too large.
 int cut_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass pass, int32_t dtype,
                gasloc::LinearArgs* a) {
   if (!linear_tiles(c.n, row_ptr, pass, 128, a)) return 0;

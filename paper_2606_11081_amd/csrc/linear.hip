@@ -14,7 +14,7 @@
 // (1020 TFLOP/s); input gradient of 2048 -> 2048 under fp32 weights 264 us (1040);
 // weight gradient of n = 8, 30011 ragged rows 227 us (1110).  Small products wait
 // for their first loads and the launches: n = 8, 256 rows each, 1024 -> 1024 in bf16
-// 11 us; weight gradient of n = 3, 1111 rows, 513 x 257 in fp32 16 us, in two launches.  A 2048-deep loop
+// 11 us; weight gradient of n = 3, 1111 rows, 513 x 257 in fp32 15 us, in two launches.  A 2048-deep loop
 // alone runs at 1100 to 1200.  The loads bound it: without those of the loop it
 // ran at 1340 to 1510, with all of them hitting L2 at 1230 to 1330, while the
 // place of stores, loads and waits among the products changes less than 2%.  A
