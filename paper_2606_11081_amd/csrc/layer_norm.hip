@@ -140,16 +140,16 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES* kWave) void k_layer_norm_
     const float mean = a.stats[2 * static_cast<int64_t>(t)], rstd = a.stats[2 * static_cast<int64_t>(t) + 1];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      float v[V], d[V] = {};  // columns behind the row count nothing in h, and xh is not used there
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = mean;
+      float v[V] = {}, d[V] = {};
       if (c0 + j * kStep < a.width) {
         load_row<AT, V, true>(a.x, static_cast<int64_t>(t) * a.x_ld + c0 + j * kStep, left(j), v);
         load_row<AT, V, true>(a.dout, static_cast<int64_t>(t) * a.dout_ld + c0 + j * kStep, left(j), d);
       }
+      // Columns behind the row count nothing: h and xh are zero there (0 * xh would be NaN if mean * rstd overflowed).
+      const int inside = a.width - (c0 + j * kStep);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[j * V + e] = v[e];
+        x[j * V + e] = (WHOLE ? 0 : e) < inside ? v[e] : mean;
         h[j * V + e] = d[e];
       }
     }
