@@ -22,9 +22,12 @@ using gasloc::Spans;
 
 namespace {
 
-// A launch holds fewer than 2^32 threads; at most 16 of them go with a row.
+// A launch holds fewer than 2^32 threads.  Where there are many rows, at most 16 of them go with a row in the lookup,
+// the sort, the merges, the sums and the norm's backward pass; the launches that may need more are checked: linear
+// layers by kMaxGroups, the norm's forward pass and the zeroing of tables by check_launch.
 constexpr int64_t kMaxRows = int64_t(1) << 27;
-constexpr int64_t kMaxGroups = 0xffffffffll / 512;  // of a linear layer's launch
+constexpr int64_t kMaxThreads = 0xffffffffll;
+constexpr int64_t kMaxGroups = kMaxThreads / 512;  // of a linear layer's launch
 constexpr int64_t kMaxLd = int64_t(1) << 21;
 
 // Nothing but a status leaves the library: building a message may run out of memory.
@@ -72,6 +75,10 @@ std::string check_act(const char* what, const void* p, int64_t ld, int64_t cols,
     return format("%s is not aligned to its elements", what);
   if (ld < cols || ld >= kMaxLd) return format("%s: row length must be in [%lld, 2^21)", what, (long long)cols);
   return "";
+}
+
+std::string check_launch(const char* what, int64_t groups, int64_t threads) {
+  return groups * threads > kMaxThreads ? format("%s too large for one launch", what) : std::string();
 }
 
 // A result may take the place of an operand if their rows are the same.
@@ -424,6 +431,13 @@ gasloc_status gasloc_embedding_grad(gasloc_ctx* c, int64_t begin, int32_t vocab,
     const EmbeddingSpace space = embedding_space(n, width, row_ptr);
     CHECK(c, check_workspace(workspace, workspace_bytes, space.bytes));
     if (rows == 0 && accumulate) return GASLOC_OK;
+    // Rows without tokens are zeroed about 16 KB to a workgroup (or four rows), in the order of the rows: what is
+    // written at any time is one stretch of memory (n = 16 tables of 32000 x 1024, 1 MB each: 454 us; 256 KB: 436;
+    // 16 KB: 358).
+    const int64_t fill_rows = std::min<int64_t>(gasloc::kMaxChunk, std::max<int64_t>(4, 4096 / width));
+    const int64_t chunk = sum_chunk(rows);
+    const Spans chunks = item_spans(n, row_ptr, chunk);
+    CHECK(c, check_launch("table", chunks.begin[n] + (accumulate ? 0 : n * ((vocab + fill_rows - 1) / fill_rows)), 256));
     char* ws = static_cast<char*>(workspace);
     const auto keys = [&](int k) { return reinterpret_cast<uint32_t*>(ws + space.keys[k]); };
     const auto pos = [&](int k) { return reinterpret_cast<int32_t*>(ws + space.pos[k]); };
@@ -468,14 +482,11 @@ gasloc_status gasloc_embedding_grad(gasloc_ctx* c, int64_t begin, int32_t vocab,
     a.vocab = vocab;
     a.width = width;
     a.n = n;
-    a.chunk = static_cast<int32_t>(sum_chunk(rows));
+    a.chunk = static_cast<int32_t>(chunk);
     a.accumulate = accumulate;
     a.rows = row_spans(n, row_ptr);
-    a.chunks = item_spans(n, row_ptr, a.chunk);
-    // Rows without tokens are zeroed about 16 KB to a workgroup (or four rows), in the order of the rows: what is
-    // written at any time is one stretch of memory (n = 16 tables of 32000 x 1024, 1 MB each: 454 us; 256 KB: 436;
-    // 16 KB: 358).
-    a.fill_rows = static_cast<int32_t>(std::min<int64_t>(gasloc::kMaxChunk, std::max<int64_t>(4, 4096 / width)));
+    a.chunks = chunks;
+    a.fill_rows = static_cast<int32_t>(fill_rows);
     HIP_TRY(c, gasloc::launch_embedding_sums(a, dtype, c->stream));
     if (rows > a.chunk) HIP_TRY(c, gasloc::launch_embedding_join(a, c->stream));
     return GASLOC_OK;
@@ -513,6 +524,7 @@ gasloc_status gasloc_layer_norm(gasloc_ctx* c, int64_t gain, int64_t bias, int32
     a.tile_rows = static_cast<int32_t>(forward_tile_rows(*c, rows, gasloc::norm_waves(width)));
     a.rows = row_spans(c->n, row_ptr);
     a.tiles = item_spans(c->n, row_ptr, a.tile_rows);
+    CHECK(c, check_launch("rows", a.tiles.begin[c->n], std::max(4, gasloc::norm_waves(width)) * 64));
     DeviceGuard guard(c->device);
     HIP_TRY(c, gasloc::launch_layer_norm(a, c->hp.param_dtype, dtype, whole_vectors(width, dtype), c->stream));
     return GASLOC_OK;
