@@ -106,6 +106,7 @@ _SIGNATURES = {
 }
 
 _lib = None
+_workers = {}  # workers of every context that gasloc_init made
 
 
 def library():
@@ -183,6 +184,7 @@ def gasloc_init(n, P, topology, hparams, x, y, m, v, u, zp, ld, stream=None):
     st = library().gasloc_init(int(n), int(P), ctypes.byref(topology), ctypes.byref(hparams),
                                ctypes.byref(bufs), stream, ctypes.byref(out))
     _check(st)
+    _workers[out.value] = int(n)
     return out.value
 
 
@@ -336,9 +338,12 @@ def gasloc_stream_probe(reads_f32, reads_bf16, writes_f32, writes_bf16, src, dst
     _check(st)
 
 
-def _row_ptr(a):
-    """row_ptr as (an int64 array that is kept alive, its address)."""
+def _row_ptr(ctx, a):
+    """row_ptr as (an int64 array that is kept alive, its address); the library reads a number per worker and one more."""
     a = np.ascontiguousarray(a, dtype=np.int64)
+    n = _workers.get(ctx)
+    if n is not None and a.shape != (n + 1,):
+        raise ValueError("row_ptr needs %d numbers" % (n + 1))
     return a, a.ctypes.data
 
 
@@ -365,7 +370,7 @@ def _act_code(dtype):
 
 
 def gasloc_embedding(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, out, out_ld):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_embedding(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
                                       _act(dtype), _dev(out), int(out_ld)), ctx)
     del keep
@@ -373,7 +378,7 @@ def gasloc_embedding(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, ou
 
 def gasloc_embedding_grad(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, dout, dout_ld, grads, grad_ld,
                           accumulate, workspace, workspace_bytes):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_embedding_grad(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
                                            _act(dtype), _dev(dout), int(dout_ld), _dev(grads), int(grad_ld),
                                            int(accumulate), _dev(workspace), int(workspace_bytes)), ctx)
@@ -381,7 +386,7 @@ def gasloc_embedding_grad(ctx, begin, vocab, width, scale, row_ptr, tokens, dtyp
 
 
 def gasloc_embedding_grad_workspace(ctx, width, row_ptr):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     out = ctypes.c_size_t()
     _check(library().gasloc_embedding_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
     del keep
@@ -389,7 +394,7 @@ def gasloc_embedding_grad_workspace(ctx, width, row_ptr):
 
 
 def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out, out_ld, stats=None):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_layer_norm(ctx, int(gain), int(bias), int(width), float(eps), rp, _dev(x), int(x_ld),
                                        _act(dtype), _dev(out), int(out_ld), _dev(stats)), ctx)
     del keep
@@ -397,7 +402,7 @@ def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out,
 
 def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout, dout_ld, dtype, dx, dx_ld, grads,
                            grad_ld, accumulate, workspace, workspace_bytes):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_layer_norm_grad(ctx, int(gain), int(bias), int(width), rp, _dev(x), int(x_ld),
                                             _dev(stats), _dev(dout), int(dout_ld), _act(dtype), _dev(dx), int(dx_ld),
                                             _dev(grads), int(grad_ld), int(accumulate), _dev(workspace),
@@ -406,7 +411,7 @@ def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout
 
 
 def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     out = ctypes.c_size_t()
     _check(library().gasloc_layer_norm_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
     del keep
@@ -415,7 +420,7 @@ def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
 
 def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtype, out, out_ld, workspace=None,
                   workspace_bytes=0):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_linear(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x), int(x_ld),
                                    _act(dtype), _dev(out), int(out_ld), _dev(workspace), int(workspace_bytes)), ctx)
     del keep
@@ -423,7 +428,7 @@ def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtyp
 
 def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, dout, dout_ld, dtype, dx, dx_ld,
                              workspace=None, workspace_bytes=0):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_linear_grad_input(ctx, int(weight), int(out_features), int(in_features), rp, _dev(dout),
                                               int(dout_ld), _act(dtype), _dev(dx), int(dx_ld), _dev(workspace),
                                               int(workspace_bytes)), ctx)
@@ -432,7 +437,7 @@ def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, do
 
 def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dout, dout_ld, dtype, grads,
                               grad_ld, accumulate, workspace, workspace_bytes):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     _check(library().gasloc_linear_grad_weight(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x),
                                                int(x_ld), _dev(dout), int(dout_ld), _act(dtype), _dev(grads),
                                                int(grad_ld), int(accumulate), _dev(workspace),
@@ -441,7 +446,7 @@ def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x
 
 
 def gasloc_linear_workspace(ctx, out_features, in_features, row_ptr, dtype):
-    keep, rp = _row_ptr(row_ptr)
+    keep, rp = _row_ptr(ctx, row_ptr)
     out = ctypes.c_size_t()
     _check(library().gasloc_linear_workspace(ctx, int(out_features), int(in_features), rp, _act(dtype),
                                              ctypes.byref(out)))
@@ -460,6 +465,7 @@ def gasloc_build_info():
 
 
 def gasloc_destroy(ctx):
+    _workers.pop(ctx, None)
     library().gasloc_destroy(ctx)
 
 

@@ -1,0 +1,52 @@
+"""The binding of the layer calls (no GPU): arguments that must not reach the library."""
+import pytest
+
+import paper_2606_11081_amd as g
+
+CTX = 0x1000  # no context: nothing may be called with it
+
+
+def functions(row_ptr, **changes):
+    """The module functions by name, with good arguments for a context of three workers but for the changes."""
+    a = dict(vocab=8, width=4, out=4, inp=4)
+    a.update(changes)
+    v, w, m, k, p = a["vocab"], a["width"], a["out"], a["inp"], 0x30000000
+    f = g.gasloc
+    return {
+        "embedding": lambda: f.gasloc_embedding(CTX, 0, v, w, 1.0, row_ptr, p, "f32", p, 4),
+        "embedding_grad": lambda: f.gasloc_embedding_grad(CTX, 0, v, w, 1.0, row_ptr, p, "f32", p, 4, p, 64, 0, p, 1 << 20),
+        "embedding_grad_workspace": lambda: f.gasloc_embedding_grad_workspace(CTX, w, row_ptr),
+        "layer_norm": lambda: f.gasloc_layer_norm(CTX, 0, 4, w, 1e-5, row_ptr, p, 4, "f32", p, 4),
+        "layer_norm_grad": lambda: f.gasloc_layer_norm_grad(CTX, 0, 4, w, row_ptr, p, 4, p, p, 4, "f32", p, 4, p, 64, 0, p,
+                                                            1 << 20),
+        "layer_norm_grad_workspace": lambda: f.gasloc_layer_norm_grad_workspace(CTX, w, row_ptr),
+        "linear": lambda: f.gasloc_linear(CTX, 0, m, k, row_ptr, p, 4, "f32", p, 4),
+        "linear_grad_input": lambda: f.gasloc_linear_grad_input(CTX, 0, m, k, row_ptr, p, 4, "f32", p, 4),
+        "linear_grad_weight": lambda: f.gasloc_linear_grad_weight(CTX, 0, m, k, row_ptr, p, 4, p, 4, "f32", p, 64, 0, None,
+                                                                  0),
+        "linear_workspace": lambda: f.gasloc_linear_workspace(CTX, m, k, row_ptr, "f32"),
+    }
+
+
+NAMES = sorted(functions(None))
+
+
+@pytest.mark.parametrize("row_ptr", [[0, 1, 2], [0, 1, 2, 3, 4], [], [[0, 1, 2, 3]], 0])
+@pytest.mark.parametrize("name", NAMES)
+def test_row_ptr_of_another_length(monkeypatch, name, row_ptr):
+    """The library would read behind the end of a shorter one."""
+    monkeypatch.setitem(g.gasloc._workers, CTX, 3)
+    with pytest.raises(ValueError, match="row_ptr needs 4 numbers"):
+        functions(row_ptr)[name]()
+
+
+def test_contexts_are_forgotten(monkeypatch):
+    class Library:
+        gasloc_destroy = staticmethod(lambda ctx: None)
+
+    monkeypatch.setattr(g.gasloc, "library", lambda: Library)
+    monkeypatch.setitem(g.gasloc._workers, CTX, 3)
+    g.gasloc_destroy(CTX)
+    assert CTX not in g.gasloc._workers
+    g.gasloc_destroy(CTX)
+    g.gasloc_destroy(None)
