@@ -339,12 +339,21 @@ def gasloc_stream_probe(reads_f32, reads_bf16, writes_f32, writes_bf16, src, dst
 
 
 def _row_ptr(ctx, a):
-    """row_ptr as (an int64 array that is kept alive, its address); the library reads a number per worker and one more."""
+    """row_ptr as (an int64 array that is kept alive, its address).  The library reads a number per worker and one
+    more."""
     a = np.ascontiguousarray(a, dtype=np.int64)
     n = _workers.get(ctx)
     if n is not None and a.shape != (n + 1,):
         raise ValueError("row_ptr needs %d numbers" % (n + 1))
     return a, a.ctypes.data
+
+
+def _int32(v):
+    """v as an int that the library's int32 holds (ctypes would pass the low 32 bits of a larger one)."""
+    v = int(v)
+    if not -0x80000000 <= v < 0x80000000:
+        raise ValueError("%d does not fit in 32 bits" % v)
+    return v
 
 
 # Layers over the workers' rows (include/gasloc_layers.h).  row_ptr: n + 1 host numbers; activations, tokens,
@@ -371,31 +380,32 @@ def _act_code(dtype):
 
 def gasloc_embedding(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, out, out_ld):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_embedding(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
-                                      _act(dtype), _dev(out), int(out_ld)), ctx)
+    _check(library().gasloc_embedding(ctx, int(begin), _int32(vocab), _int32(width), float(scale), rp,
+                                      _dev(tokens), _act(dtype), _dev(out), int(out_ld)), ctx)
     del keep
 
 
 def gasloc_embedding_grad(ctx, begin, vocab, width, scale, row_ptr, tokens, dtype, dout, dout_ld, grads, grad_ld,
                           accumulate, workspace, workspace_bytes):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_embedding_grad(ctx, int(begin), int(vocab), int(width), float(scale), rp, _dev(tokens),
-                                           _act(dtype), _dev(dout), int(dout_ld), _dev(grads), int(grad_ld),
-                                           int(accumulate), _dev(workspace), int(workspace_bytes)), ctx)
+    _check(library().gasloc_embedding_grad(ctx, int(begin), _int32(vocab), _int32(width), float(scale), rp,
+                                           _dev(tokens), _act(dtype), _dev(dout), int(dout_ld), _dev(grads),
+                                           int(grad_ld), _int32(accumulate), _dev(workspace), int(workspace_bytes)),
+           ctx)
     del keep
 
 
 def gasloc_embedding_grad_workspace(ctx, width, row_ptr):
     keep, rp = _row_ptr(ctx, row_ptr)
     out = ctypes.c_size_t()
-    _check(library().gasloc_embedding_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
+    _check(library().gasloc_embedding_grad_workspace(ctx, _int32(width), rp, ctypes.byref(out)))
     del keep
     return out.value
 
 
 def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out, out_ld, stats=None):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_layer_norm(ctx, int(gain), int(bias), int(width), float(eps), rp, _dev(x), int(x_ld),
+    _check(library().gasloc_layer_norm(ctx, int(gain), int(bias), _int32(width), float(eps), rp, _dev(x), int(x_ld),
                                        _act(dtype), _dev(out), int(out_ld), _dev(stats)), ctx)
     del keep
 
@@ -403,9 +413,9 @@ def gasloc_layer_norm(ctx, gain, bias, width, eps, row_ptr, x, x_ld, dtype, out,
 def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout, dout_ld, dtype, dx, dx_ld, grads,
                            grad_ld, accumulate, workspace, workspace_bytes):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_layer_norm_grad(ctx, int(gain), int(bias), int(width), rp, _dev(x), int(x_ld),
+    _check(library().gasloc_layer_norm_grad(ctx, int(gain), int(bias), _int32(width), rp, _dev(x), int(x_ld),
                                             _dev(stats), _dev(dout), int(dout_ld), _act(dtype), _dev(dx), int(dx_ld),
-                                            _dev(grads), int(grad_ld), int(accumulate), _dev(workspace),
+                                            _dev(grads), int(grad_ld), _int32(accumulate), _dev(workspace),
                                             int(workspace_bytes)), ctx)
     del keep
 
@@ -413,7 +423,7 @@ def gasloc_layer_norm_grad(ctx, gain, bias, width, row_ptr, x, x_ld, stats, dout
 def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
     keep, rp = _row_ptr(ctx, row_ptr)
     out = ctypes.c_size_t()
-    _check(library().gasloc_layer_norm_grad_workspace(ctx, int(width), rp, ctypes.byref(out)))
+    _check(library().gasloc_layer_norm_grad_workspace(ctx, _int32(width), rp, ctypes.byref(out)))
     del keep
     return out.value
 
@@ -421,26 +431,27 @@ def gasloc_layer_norm_grad_workspace(ctx, width, row_ptr):
 def gasloc_linear(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dtype, out, out_ld, workspace=None,
                   workspace_bytes=0):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_linear(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x), int(x_ld),
-                                   _act(dtype), _dev(out), int(out_ld), _dev(workspace), int(workspace_bytes)), ctx)
+    _check(library().gasloc_linear(ctx, int(weight), _int32(out_features), _int32(in_features), rp, _dev(x),
+                                   int(x_ld), _act(dtype), _dev(out), int(out_ld), _dev(workspace),
+                                   int(workspace_bytes)), ctx)
     del keep
 
 
 def gasloc_linear_grad_input(ctx, weight, out_features, in_features, row_ptr, dout, dout_ld, dtype, dx, dx_ld,
                              workspace=None, workspace_bytes=0):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_linear_grad_input(ctx, int(weight), int(out_features), int(in_features), rp, _dev(dout),
-                                              int(dout_ld), _act(dtype), _dev(dx), int(dx_ld), _dev(workspace),
-                                              int(workspace_bytes)), ctx)
+    _check(library().gasloc_linear_grad_input(ctx, int(weight), _int32(out_features), _int32(in_features), rp,
+                                              _dev(dout), int(dout_ld), _act(dtype), _dev(dx), int(dx_ld),
+                                              _dev(workspace), int(workspace_bytes)), ctx)
     del keep
 
 
 def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x, x_ld, dout, dout_ld, dtype, grads,
                               grad_ld, accumulate, workspace, workspace_bytes):
     keep, rp = _row_ptr(ctx, row_ptr)
-    _check(library().gasloc_linear_grad_weight(ctx, int(weight), int(out_features), int(in_features), rp, _dev(x),
-                                               int(x_ld), _dev(dout), int(dout_ld), _act(dtype), _dev(grads),
-                                               int(grad_ld), int(accumulate), _dev(workspace),
+    _check(library().gasloc_linear_grad_weight(ctx, int(weight), _int32(out_features), _int32(in_features), rp,
+                                               _dev(x), int(x_ld), _dev(dout), int(dout_ld), _act(dtype), _dev(grads),
+                                               int(grad_ld), _int32(accumulate), _dev(workspace),
                                                int(workspace_bytes)), ctx)
     del keep
 
@@ -448,7 +459,7 @@ def gasloc_linear_grad_weight(ctx, weight, out_features, in_features, row_ptr, x
 def gasloc_linear_workspace(ctx, out_features, in_features, row_ptr, dtype):
     keep, rp = _row_ptr(ctx, row_ptr)
     out = ctypes.c_size_t()
-    _check(library().gasloc_linear_workspace(ctx, int(out_features), int(in_features), rp, _act(dtype),
+    _check(library().gasloc_linear_workspace(ctx, _int32(out_features), _int32(in_features), rp, _act(dtype),
                                              ctypes.byref(out)))
     del keep
     return out.value
@@ -666,7 +677,7 @@ class GASLoC:
         code = _act(out.dtype if out is not None else self.bufs["x"].dtype if dtype is None else dtype)
         out, ld = self._out("out", out, rows, width, torch.bfloat16 if code == GASLOC_BF16 else torch.float32, device)
         self._tokens(tokens, rows, device)
-        self._run("gasloc_embedding", (tokens, out), int(table), int(vocab), int(width), float(scale),
+        self._run("gasloc_embedding", (tokens, out), int(table), _int32(vocab), int(width), float(scale),
                   rp.tobytes(), tokens.data_ptr(), code, out.data_ptr(), ld)
         return out
 
@@ -679,8 +690,8 @@ class GASLoC:
         self._tokens(tokens, rows, device)
         kept, ws, size = self._workspace(workspace, device, "gasloc_embedding_grad_workspace", int(width),
                                          rp.tobytes())
-        self._run("gasloc_embedding_grad", (tokens, dout, grads, *kept), int(table), int(vocab), int(width), float(scale),
-                  rp.tobytes(), tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld, grads.data_ptr(), gld,
+        self._run("gasloc_embedding_grad", (tokens, dout, grads, *kept), int(table), _int32(vocab), int(width),
+                  float(scale), rp.tobytes(), tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld, grads.data_ptr(), gld,
                   bool(accumulate), ws, size)
 
     def layer_norm(self, gain, bias, width, x, row_ptr, eps=1e-5, out=None, stats=None):

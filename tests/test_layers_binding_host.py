@@ -14,16 +14,17 @@ def functions(row_ptr, **changes):
     f = g.gasloc
     return {
         "embedding": lambda: f.gasloc_embedding(CTX, 0, v, w, 1.0, row_ptr, p, "f32", p, 4),
-        "embedding_grad": lambda: f.gasloc_embedding_grad(CTX, 0, v, w, 1.0, row_ptr, p, "f32", p, 4, p, 64, 0, p, 1 << 20),
+        "embedding_grad": lambda: f.gasloc_embedding_grad(CTX, 0, v, w, 1.0, row_ptr, p, "f32", p, 4, p, 64, 0, p,
+                                                          1 << 20),
         "embedding_grad_workspace": lambda: f.gasloc_embedding_grad_workspace(CTX, w, row_ptr),
         "layer_norm": lambda: f.gasloc_layer_norm(CTX, 0, 4, w, 1e-5, row_ptr, p, 4, "f32", p, 4),
-        "layer_norm_grad": lambda: f.gasloc_layer_norm_grad(CTX, 0, 4, w, row_ptr, p, 4, p, p, 4, "f32", p, 4, p, 64, 0, p,
-                                                            1 << 20),
+        "layer_norm_grad": lambda: f.gasloc_layer_norm_grad(CTX, 0, 4, w, row_ptr, p, 4, p, p, 4, "f32", p, 4, p, 64, 0,
+                                                            p, 1 << 20),
         "layer_norm_grad_workspace": lambda: f.gasloc_layer_norm_grad_workspace(CTX, w, row_ptr),
         "linear": lambda: f.gasloc_linear(CTX, 0, m, k, row_ptr, p, 4, "f32", p, 4),
         "linear_grad_input": lambda: f.gasloc_linear_grad_input(CTX, 0, m, k, row_ptr, p, 4, "f32", p, 4),
-        "linear_grad_weight": lambda: f.gasloc_linear_grad_weight(CTX, 0, m, k, row_ptr, p, 4, p, 4, "f32", p, 64, 0, None,
-                                                                  0),
+        "linear_grad_weight": lambda: f.gasloc_linear_grad_weight(CTX, 0, m, k, row_ptr, p, 4, p, 4, "f32", p, 64, 0,
+                                                                  None, 0),
         "linear_workspace": lambda: f.gasloc_linear_workspace(CTX, m, k, row_ptr, "f32"),
     }
 
@@ -50,3 +51,37 @@ def test_contexts_are_forgotten(monkeypatch):
     assert CTX not in g.gasloc._workers
     g.gasloc_destroy(CTX)
     g.gasloc_destroy(None)
+
+
+@pytest.mark.parametrize("value", [(1 << 32) + 4, 1 << 31, -(1 << 31) - 1, -(1 << 32) + 4])
+@pytest.mark.parametrize("key", ["vocab", "width", "out", "inp"])
+def test_sizes_beyond_32_bits(monkeypatch, key, value):
+    """Their low 32 bits may be a size that the library takes."""
+    monkeypatch.setitem(g.gasloc._workers, CTX, 3)
+    uses = {"vocab": ("embedding", "embedding_grad"), "out": ("linear",), "inp": ("linear",),
+            "width": ("embedding", "layer_norm")}[key]
+    hit = [n for n in NAMES if n.startswith(uses) and (key != "vocab" or "workspace" not in n)]
+    assert hit
+    for name in hit:
+        with pytest.raises(ValueError, match="does not fit in 32 bits"):
+            functions([0, 1, 2, 3], **{key: value})[name]()
+
+
+@pytest.mark.parametrize("vocab", [(1 << 32) + 8, -(1 << 32) + 8])
+def test_methods_with_a_vocabulary_beyond_32_bits(monkeypatch, vocab):
+    import torch
+
+    run = g.GASLoC.__new__(g.GASLoC)
+    run.n, run.P, run.bufs = 3, 64, dict(x=torch.zeros(3, 64))
+    called = []
+    monkeypatch.setattr(run, "_run", lambda *a: called.append(a), raising=False)
+    monkeypatch.setattr(run, "_workspace", lambda *a: ((), None, 0), raising=False)
+    tokens, rows, grads = torch.zeros(3, dtype=torch.int32), torch.zeros(3, 4), torch.zeros(3, 64)
+    run.embedding(0, 8, 4, tokens, [0, 1, 2, 3])
+    run.embedding_grad(0, 8, 4, tokens, [0, 1, 2, 3], rows, grads)
+    assert [a[0] for a in called] == ["gasloc_embedding", "gasloc_embedding_grad"]
+    with pytest.raises(ValueError, match="does not fit in 32 bits"):
+        run.embedding(0, vocab, 4, tokens, [0, 1, 2, 3])
+    with pytest.raises(ValueError, match="does not fit in 32 bits"):
+        run.embedding_grad(0, vocab, 4, tokens, [0, 1, 2, 3], rows, grads)
+    assert len(called) == 2
