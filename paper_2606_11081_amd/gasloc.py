@@ -563,14 +563,23 @@ class GASLoC:
         with torch.cuda.stream(self.stream):
             self.bufs["x"][:, : self.P].copy_(x0.to(self.bufs["x"].dtype).view(1, -1).expand(self.n, -1))
 
+    def _grad_ld(self, grads):
+        """Elements from one row of grads to the next, which in a view of some columns are more than it shows."""
+        if len(grads.shape) != 2 or grads.shape[0] < 2:
+            return grads.shape[1]
+        ld, step = grads.stride()
+        if step != 1:
+            raise ValueError("the rows of grads must be contiguous")
+        return ld
+
     def local_step(self, grads, lr, active=None):
-        gasloc_local_step(self.ctx, grads, grads.shape[1], active, lr)
+        gasloc_local_step(self.ctx, grads, self._grad_ld(grads), active, lr)
 
     def gossip_round(self, t, W=None):
         gasloc_gossip_round(self.ctx, W, t)
 
     def local_step_gossip_round(self, grads, lr, t, active=None, W=None):
-        gasloc_local_step_gossip_round(self.ctx, grads, grads.shape[1], active, lr, W, t)
+        gasloc_local_step_gossip_round(self.ctx, grads, self._grad_ld(grads), active, lr, W, t)
 
     def consensus_error(self):
         return gasloc_consensus_error(self.ctx)
@@ -691,8 +700,8 @@ class GASLoC:
         kept, ws, size = self._workspace(workspace, device, "gasloc_embedding_grad_workspace", int(width),
                                          rp.tobytes())
         self._run("gasloc_embedding_grad", (tokens, dout, grads, *kept), int(table), _int32(vocab), int(width),
-                  float(scale), rp.tobytes(), tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld, grads.data_ptr(), gld,
-                  bool(accumulate), ws, size)
+                  float(scale), rp.tobytes(), tokens.data_ptr(), _act(dout.dtype), dout.data_ptr(), ld,
+                  grads.data_ptr(), gld, bool(accumulate), ws, size)
 
     def layer_norm(self, gain, bias, width, x, row_ptr, eps=1e-5, out=None, stats=None):
         """(out, stats): the normalised rows (gain and bias at these columns; bias None: none) and every

@@ -61,3 +61,32 @@ def test_functions_are_the_methods(params, act):
     assert same(d, d)
     assert run.ctx in g.gasloc._workers
     run.close()
+
+
+def test_gradients_in_columns_of_a_larger_tensor():
+    """The layers write them and the local steps read them as if the tensor held nothing else."""
+    import torch
+
+    n, width = 3, 16
+    cols = width * width
+    ptr = [0, 4, 4, 13]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    start = torch.empty(cols, device="cuda").normal_(generator=gen)
+    x, d = (torch.empty((13, width), device="cuda").normal_(generator=gen) for _ in range(2))
+    states = []
+    for view in (False, True):
+        run = g.GASLoC(n, cols, topology="ring")
+        run.set_params(start)
+        grads = torch.full((n, 100 + cols + 60), float("nan"), device="cuda")[:, 100:100 + cols] if view else \
+            torch.full((n, cols), float("nan"), device="cuda")
+        for t in range(2):
+            run.linear_grad_weight(0, width, width, x, d, ptr, grads)
+            run.local_step(grads, 1e-2)
+            run.linear_grad_weight(0, width, width, d, x, ptr, grads)
+            run.local_step_gossip_round(grads, 1e-2, t)
+        torch.cuda.synchronize()
+        states.append([run.bufs[k][:, :cols].clone() for k in ("x", "m", "v", "u", "zp")])
+        run.close()
+    for a, b in zip(*states):
+        assert bool(torch.isfinite(a).all()) and torch.equal(a, b)

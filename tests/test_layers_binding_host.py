@@ -85,3 +85,25 @@ def test_methods_with_a_vocabulary_beyond_32_bits(monkeypatch, vocab):
     with pytest.raises(ValueError, match="does not fit in 32 bits"):
         run.embedding_grad(0, vocab, 4, tokens, [0, 1, 2, 3], rows, grads)
     assert len(called) == 2
+
+
+def test_local_steps_take_the_rows_of_a_view(monkeypatch):
+    """Gradients in some columns of a larger tensor, as the layer calls take them, lie that tensor's rows apart."""
+    import torch
+
+    run = g.GASLoC.__new__(g.GASLoC)
+    run.ctx, run.n, run.P, run.bufs = None, 3, 8, dict(x=torch.zeros(3, 8))
+    got = []
+    monkeypatch.setattr(g.gasloc, "gasloc_local_step", lambda ctx, grads, ld, active, lr: got.append(ld))
+    monkeypatch.setattr(g.gasloc, "gasloc_local_step_gossip_round",
+                        lambda ctx, grads, ld, active, lr, W, t: got.append(ld))
+    whole = torch.zeros(3, 20)
+    for grads, ld in ((whole, 20), (whole[:, :8], 20), (whole[:, 4:12], 20), (torch.zeros(6, 8)[::2], 16),
+                      (torch.zeros(1, 8).expand(3, 8), 0), (torch.zeros(1, 8), 8)):
+        run.local_step(grads, 1e-3)
+        run.local_step_gossip_round(grads, 1e-3, 0)
+        assert got == [ld, ld]  # the library refuses rows of 0
+        del got[:]
+    with pytest.raises(ValueError, match="contiguous"):
+        run.local_step(torch.zeros(8, 3).t(), 1e-3)
+    assert not got
