@@ -17,7 +17,11 @@
  *     in_features] takes out_features * in_features columns).  Worker i's
  *     weights are read from its live iterate: row i of y if it took a local
  *     step since the last round, else row i of x.  Which of the two is decided
- *     when the call is made, also for a call that is recorded in a graph.
+ *     when the call is made, also for a call that is recorded in a graph: a
+ *     replay reads the rows that were live at the recording.  It gives what an
+ *     eager call would while the same workers have stepped since the last round
+ *     as then, so a program with several local steps per round records its step
+ *     twice, once before and once after the first of them.
  *   - Activations: device memory, row t at offset t * ld elements (ld >= the
  *     row's length, < 2^21), dtype GASLOC_F32 or GASLOC_BF16, aligned to the
  *     element.  Types go together as (parameters, activations) = (F32, F32),
@@ -29,8 +33,8 @@
  *     accumulate = 1 adds to them.  Other columns are left as they are.
  *   - Sums, means and products are taken in fp32 (never in fewer bits), and
  *     rounded once, to nearest even, where the result is BF16.  Every sum has
- *     an order that depends on the sizes alone: the same call gives the same
- *     bits again.
+ *     an order that depends on the sizes, the types, the alignment of rows and
+ *     weights and the GPU alone: the same call gives the same bits again.
  *   - All work is enqueued on the context's stream; no call waits, allocates or
  *     copies, so each may be recorded in a graph (of a context whose stream is not
  *     the default one).  Workspaces are the caller's
@@ -42,9 +46,10 @@
  *     get for a gradient is not used by their skipped steps.
  *   - Vector accesses are taken where rows and weights begin on 16-byte
  *     boundaries and row lengths are a multiple of 8 (BF16) or 4 (F32)
- *     elements; anything else is served too, at half to three quarters of the
- *     rate in linear layers.
- *   - Errors: EINVAL (checked before any device work), EDEVICE, ESTATE.
+ *     elements (features of linear layers: of 8 in either type); anything else
+ *     is served too, at half to three quarters of the rate in linear layers.
+ *   - Errors: EINVAL (checked before any device work; also for what one launch of
+ *     fewer than 2^32 threads cannot hold), ENOMEM (host memory), EDEVICE, ESTATE.
  */
 #ifndef GASLOC_LAYERS_H
 #define GASLOC_LAYERS_H
@@ -70,7 +75,7 @@ gasloc_status gasloc_embedding(gasloc_ctx *ctx, int64_t begin, int32_t vocab, in
  *   grads_i[begin + k * width ..] (+)= scale * sum over t with tokens[t] = k of dout[t, :].
  * The tokens are sorted first (stable), so that every table row is written
  * once, by sums that go over its tokens in order.  Padding tokens contribute
- * nothing.  Enqueues three kernels, and one more for each factor of 8 by which
+ * nothing.  Enqueues three kernels (fewer with few rows), and one more for each factor of 8 by which
  * the longest worker exceeds 8192 rows.  workspace: at least
  * gasloc_embedding_grad_workspace bytes. */
 gasloc_status gasloc_embedding_grad(gasloc_ctx *ctx, int64_t begin, int32_t vocab, int32_t width, float scale,

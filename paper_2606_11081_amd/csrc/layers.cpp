@@ -297,7 +297,9 @@ int cut_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass p
 // Splits the sums of a product whose tiles are fewer than two per CU, so that about two workgroups per CU share the
 // steps of k, if that saves more steps than the parts cost: the join's launch takes about as long as 16 steps (4 us),
 // and writing and adding a megabyte of parts as 2.  bf16, whole / split: n = 2, 64 rows each, 8192 -> 512 40 / 14 us;
-// n = 16, 64 rows, 1024 -> 1024 9.4 / 14.  Returns the bytes of the parts.
+// n = 16, 64 rows, 1024 -> 1024 9.4 / 14.  Tiles are counted whatever they cost: a weight's gradient with most rows in
+// one worker is not split, and few CUs have its work (n = 8, 2048 -> 2048, 30011 rows, 95% of them in one worker: 622
+// us, spread evenly 245).  Returns the bytes of the parts.
 size_t split_linear(const gasloc_ctx& c, const int64_t* row_ptr, gasloc::LinearPass pass, int32_t dtype,
                     gasloc::LinearArgs* a) {
   const int n = c.n;
@@ -340,7 +342,8 @@ gasloc_status run_linear(gasloc_ctx* c, gasloc::LinearArgs* a, gasloc::LinearPas
   for (int i = 0; i < c->n; ++i) most = std::max(most, row_ptr[i + 1] - row_ptr[i]);
   int tile = vec && dtype == GASLOC_BF16 ? 256 : 128;
   // Few rows: the weights' way through LDS in tiles of 128 outputs leaves too few loads in flight (n = 16, one row
-  // each, 2048 -> 2048, bf16 rows, fp32 weights: 61 us against 48).
+  // each, 2048 -> 2048, bf16 rows, fp32 weights: 61 us against 48).  One worker with more rows than the others sends
+  // all of them to the tiles, which costs nothing there: 15 of one row and one of 16 take 43 us, one of 17 40.
   if (pass == gasloc::kLinearForward && most <= gasloc::kFewRows) tile = gasloc::kFewRows;
   bool fits = linear_tiles(c->n, row_ptr, pass, tile, a);
   const int64_t large = a->tiles.begin[c->n];

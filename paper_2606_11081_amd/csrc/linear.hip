@@ -10,9 +10,11 @@
 // 16-byte fragments; one whose rows run across k lies as [k][row] and is
 // transposed by the LDS read itself (bf16) or read by words (fp32).
 //
-// Measured, bf16 rows: n = 16, 32768 rows, 1024 -> 4096, bf16 weights 270 us
-// (1020 TFLOP/s); input gradient of 2048 -> 2048 under fp32 weights 264 us (1040);
-// weight gradient of n = 8, 30011 ragged rows 227 us (1110).  Small products wait
+// Measured on several cards, bf16 rows: n = 16, 32768 rows, 1024 -> 4096, bf16
+// weights 270 to 278 us (990 to 1020 TFLOP/s); input gradient of 2048 -> 2048 under
+// fp32 weights 264 to 280 us (980 to 1040); weight gradient of n = 8, 30011 ragged
+// rows 227 to 240 us (1050 to 1110).  fp32, n = 4, 1024 rows each, 2048 -> 2048: 257
+// to 261 us in each direction (132 to 134 TFLOP/s).  Small products wait
 // for their first loads and the launches: n = 8, 256 rows each, 1024 -> 1024 in bf16
 // 11 us; weight gradient of n = 3, 1111 rows, 513 x 257 in fp32 15 us, in two launches.  A 2048-deep loop
 // alone runs at 1100 to 1200.  The loads bound it: without those of the loop it
@@ -62,9 +64,11 @@ __device__ __forceinline__ __attribute__((address_space(3))) T* lds_pointer(uint
 //
 // In LDS a KC step is [row][64 bytes], its four blocks of 16 permuted by the
 // row's place among sixteen; other bf16 steps are [k][row], blocks of 32 bytes
-// permuted by k; fp32 ones have their lines 16 bytes apart.  So neither the
-// writes nor the lanes that a fragment read serves at a time meet in a bank
-// (plain padding of 16 bytes per KC row cost as many cycles in conflicts again).
+// permuted by k; fp32 ones have their lines 16 bytes apart.  So the lanes that a
+// fragment read serves at a time do not meet in a bank (plain padding of 16 bytes
+// per KC row cost as many cycles in conflicts again).  Conflicts remain: 31% of the
+// LDS cycles of a forward pass, 18% of an input gradient's, 1% of a weight gradient's,
+// so most of them come with the writes of KC operands.
 template <int ROWS, int THREADS, bool KC, int ST, int CT, bool VEC>
 struct Operand {
   static constexpr int kSize = CT == GASLOC_BF16 ? 2 : 4;  // bytes of an element in LDS
@@ -495,7 +499,8 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
 // Lane l has output l % 16 of the weights and row l % 16 of x.  bf16 weights: of every 32 of k the 8 from 8 (l / 16)
 // on; fp32 ones: the 4 from 4 (l / 16) on and the 4 that lie 16 behind them.  Either way a load takes 64 bytes of 16
 // rows, and the other half of those lines is next, so the loads go through the caches (streaming ones took 52 us).
-// Bound by HBM: one row of n = 16, 2048 -> 2048, fp32 weights 48 us (5.6 TB/s), bf16 weights 28 (4.9).
+// Bound by HBM: one row of n = 16, 2048 -> 2048, fp32 weights 46 to 48 us (5.6 to 5.8 TB/s), bf16 weights 28 (4.9).
+// More rows take longer, 4 each 52 us and 16 each 71, where tiles of 64 take 62 (17 rows each).
 template <int PT, int AT>
 __global__ __launch_bounds__(256) void k_linear_rows(LinearArgs a) {
   constexpr int kAhead = 4;                        // 32s of k in flight
